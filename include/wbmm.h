@@ -278,6 +278,98 @@ wbmm_status wbmm_rect_backward_table(const void *x, const void *dy,
                                      int64_t C, int64_t H, int64_t W, int wh,
                                      int ww, wbmm_dtype dtype, void *stream);
 
+/* ---- Reading a map from a decoder: rotary positions and cross attention.
+ * A feature map flattened to tokens (row-major over height and width, frames
+ * outermost) is what a decoder's tokens attend to; both sides can carry
+ * positions with several axes (time, height, width).
+ *
+ * Tokens are [B, S, H, D] (batch, sequence, heads, components of a head) in
+ * `dtype`, at any strides but with contiguous components, so that a tensor
+ * can be a slice of a joint projection.  Strides are in elements and not
+ * negative.  Rows at multiples of 16 bytes (address, strides, D) move in
+ * 16-byte accesses, others element by element.  Address ranges of outputs
+ * must not overlap those of inputs or other outputs, except as tensors that
+ * share all strides between tokens and take separate parts of each token
+ * (slices of one joint tensor).
+ * The argument structs hold 8-byte fields only; set unused ones to zero. */
+typedef struct {
+  void *data;
+  int64_t stride_b, stride_s, stride_h;
+} wbmm_tokens;
+
+/* Rotary positions.  The first 2 P components of each head, P the sum of
+ * sections[0..axes), form P pairs: (i, i + P), or with `adjacent`
+ * (2 i, 2 i + 1).  The first sections[0] pairs belong to axis 0, the next
+ * sections[1] to axis 1 and so on.  A token at positions[a][b][s] turns pair i
+ * of axis a by the angle t = positions[a][b][s] * freqs[i]:
+ *   lo' = lo cos t - hi sin t,  hi' = lo sin t + hi cos t
+ * Components from 2 P on are copied.  The angle is taken in 64 bits (exact for
+ * positions below 2^29), the rotation in float32, each output rounded once.
+ * positions: device, 32- or 64-bit integers (position_bytes 4 or 8) at any
+ * strides, 0 for a broadcast; freqs: device, float32 [P], radians a position.
+ * 1 <= axes <= 4, sections not negative, 1 <= P <= 256, 2 P <= D <= 4096.
+ * y may be x itself (same address and strides).  B or S may be 0. */
+typedef struct {
+  wbmm_tokens x, y;
+  const void *positions;
+  int64_t position_bytes;
+  int64_t pos_stride_a, pos_stride_b, pos_stride_s;
+  const float *freqs;
+  int64_t axes, sections[4];
+  int64_t adjacent;
+  int64_t B, S, H, D;
+  int64_t dtype;
+} wbmm_rotary_args;
+
+wbmm_status wbmm_rotary_forward(const wbmm_rotary_args *args, void *stream);
+
+/* The gradient: y = x turned by the negative angles (x holds dy, y gets dx). */
+wbmm_status wbmm_rotary_backward(const wbmm_rotary_args *args, void *stream);
+
+/* Cross attention of Sq queries to Sk states of another length:
+ *   out[b,i,h] = sum_j p_ij v[b,j,h/G],
+ *   p_ij = exp(scale q[b,i,h].k[b,j,h/G] - lse[b,h,i])
+ * over the visible states j, with G = Hq / Hk query heads to a key head (Hk
+ * divides Hq) and lse the logarithm of the sum of the exponentials.  State j
+ * of entry b is visible if j < kv_lens[b] (device, int32 [B], or NULL: all;
+ * values are clamped to 0..Sk) and key_mask[b, j] is not zero (device, one
+ * byte each, element strides mask_stride_b and mask_stride_s, or NULL: all).
+ * What lies in states that are not visible may be anything, NaN included.
+ * Where nothing is visible, out = 0, lse = -infinity and all gradients are 0;
+ * gradients of states that are not visible are 0.
+ * q, out, dout, dq: [B,Sq,Hq,D]; k, v, dk, dv: [B,Sk,Hk,D]; lse: float32
+ * [B,Hq,Sq] contiguous.  1 <= D <= 128; scale positive and finite.  B, Sq
+ * and Sk may be 0.  16-bit types: products on the matrix cores with float32
+ * sums and a float32 softmax; p and its gradient are rounded to the type as
+ * operands of the second products.  float32: float32 products.
+ * Sums have a fixed order: results are reproducible bit for bit.
+ *
+ * workspace: device buffer of at least the size that the matching query
+ * returns for the same arguments (0: may be NULL), 16-byte aligned, any
+ * contents; calls that can run at the same time must not share one. */
+typedef struct {
+  wbmm_tokens q, k, v, out;
+  wbmm_tokens dout, dq, dk, dv; /* backward */
+  float *lse;                   /* forward: written, may be NULL; backward: read */
+  const int32_t *kv_lens;
+  const uint8_t *key_mask;
+  int64_t mask_stride_b, mask_stride_s;
+  int64_t B, Sq, Sk, Hq, Hk, D;
+  double scale;
+  int64_t dtype;
+  void *workspace;
+  int64_t workspace_bytes;
+} wbmm_cross_attention_args;
+
+/* Reads q, k, v; writes out and, unless NULL, lse. */
+size_t wbmm_cross_attention_forward_workspace_bytes(const wbmm_cross_attention_args *args);
+wbmm_status wbmm_cross_attention_forward(const wbmm_cross_attention_args *args, void *stream);
+
+/* Reads q, k, v, out, dout and lse (as the forward wrote them); overwrites
+ * dq, dk and dv. */
+size_t wbmm_cross_attention_backward_workspace_bytes(const wbmm_cross_attention_args *args);
+wbmm_status wbmm_cross_attention_backward(const wbmm_cross_attention_args *args, void *stream);
+
 /* Static description of a status code (never NULL). */
 const char *wbmm_status_string(wbmm_status s);
 

@@ -13,7 +13,10 @@ from .binding import (WBMMFunction, WBMMHierFunction, WbmmError, load_library, w
                       wbmm_relative_index, wbmm_status_string, wbmm_version,
                       wbmm_build_matrix, wbmm_dense_forward, wbmm_dense_backward_input,
                       wbmm_dense_backward_matrix, wbmm_bin_matrix, wbmm_rect_forward,
-                      wbmm_rect_backward_input, wbmm_rect_backward_table)
+                      wbmm_rect_backward_input, wbmm_rect_backward_table, WBMMRotaryFunction,
+                      WBMMCrossAttentionFunction, wbmm_rotary, wbmm_rotary_forward,
+                      wbmm_rotary_backward, wbmm_rotary_frequencies, wbmm_cross_attention,
+                      wbmm_cross_attention_forward, wbmm_cross_attention_backward)
 
 __all__ = ["wbmm_build_matrix", "wbmm_dense_forward", "wbmm_dense_backward_input",
            "wbmm_dense_backward_matrix", "wbmm_bin_matrix", "wbmm_rect_forward",
@@ -22,4 +25,6 @@ __all__ = ["wbmm_build_matrix", "wbmm_dense_forward", "wbmm_dense_backward_input
            "wbmm_hier_backward_workspace_bytes", "wbmm_backward", "wbmm_backward_noalloc",
            "wbmm_backward_input", "wbmm_backward_table", "wbmm_backward_table_workspace_bytes",
            "wbmm_backward_workspace_bytes", "wbmm_forward", "wbmm_relative_index",
-           "wbmm_status_string", "wbmm_version"]
+           "wbmm_status_string", "wbmm_version", "WBMMRotaryFunction", "WBMMCrossAttentionFunction",
+           "wbmm_rotary", "wbmm_rotary_forward", "wbmm_rotary_backward", "wbmm_rotary_frequencies",
+           "wbmm_cross_attention", "wbmm_cross_attention_forward", "wbmm_cross_attention_backward"]

@@ -14,12 +14,17 @@ Names follow the C entry points: ``wbmm_forward``, ``wbmm_backward_input``,
 ``wbmm_dense_backward_matrix``, ``wbmm_bin_matrix``, and
 ``wbmm_relative_index``, ``wbmm_status_string``.  ``wbmm_rect_*`` are WBMM for
 rectangular windows, straight from the table or with a cached matrix.
+
+``wbmm_rotary_*`` (rotary positions with several axes) and
+``wbmm_cross_attention_*`` (attention to an encoder's states of another
+length) let a decoder read feature maps.
 """
 from __future__ import annotations
 
 import ctypes
 import functools
 import os
+import struct
 
 import torch
 
@@ -42,7 +47,10 @@ EXPORTED = ("wbmm_forward", "wbmm_backward_input", "wbmm_backward_table",
             "wbmm_dense_forward", "wbmm_dense_backward_input",
             "wbmm_dense_backward_matrix", "wbmm_bin_matrix", "wbmm_rect_forward",
             "wbmm_rect_backward_input", "wbmm_rect_backward_table",
-            "wbmm_rect_backward_table_workspace_bytes", "wbmm_status_string",
+            "wbmm_rect_backward_table_workspace_bytes", "wbmm_rotary_forward",
+            "wbmm_rotary_backward", "wbmm_cross_attention_forward",
+            "wbmm_cross_attention_forward_workspace_bytes", "wbmm_cross_attention_backward",
+            "wbmm_cross_attention_backward_workspace_bytes", "wbmm_status_string",
             "wbmm_relative_index", "wbmm_version")
 
 _lib = None
@@ -106,6 +114,15 @@ def load_library(path: str = LIB_PATH):
     lib.wbmm_rect_backward_table.restype = st
     lib.wbmm_bin_matrix.argtypes = [vp, vp, i64, ci, ci, vp]
     lib.wbmm_bin_matrix.restype = st
+    for name in ("wbmm_rotary", "wbmm_cross_attention"):
+        for way in ("_forward", "_backward"):
+            # (the argument struct goes as packed bytes)
+            getattr(lib, name + way).argtypes = [ctypes.c_char_p, vp]
+            getattr(lib, name + way).restype = st
+    for way in ("forward", "backward"):
+        fn = getattr(lib, "wbmm_cross_attention_%s_workspace_bytes" % way)
+        fn.argtypes = [ctypes.c_char_p]
+        fn.restype = ctypes.c_size_t
     lib.wbmm_status_string.argtypes = [st]
     lib.wbmm_status_string.restype = ctypes.c_char_p
     lib.wbmm_relative_index.argtypes = [ci, ctypes.POINTER(ctypes.c_int32)]
@@ -580,3 +597,231 @@ class WBMMHierFunction(torch.autograd.Function):
 def wbmm_hier(x, table_g, table_l, wl):
     """Differentiable hierarchical WBMM (global windows 2 wl, local wl)."""
     return WBMMHierFunction.apply(x, table_g, table_l, wl)
+
+
+# --------------------------------- rotary positions and cross attention
+
+# wbmm_rotary_args and wbmm_cross_attention_args of include/wbmm.h
+_ROTARY_ARGS = struct.Struct("25q")
+_ATTENTION_ARGS = struct.Struct("43qd3q")
+_NO_TOKENS = (0, 0, 0, 0)
+MAX_AXES = 4
+
+
+def _tokens(t: torch.Tensor, name: str):
+    """The wbmm_tokens of a [B, S, H, D] tensor (any strides, contiguous
+    components)."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError("%s must be a torch.Tensor" % name)
+    if not t.is_cuda:
+        raise ValueError("%s must be a GPU tensor (got %s)" % (name, t.device))
+    if t.dim() != 4:
+        raise ValueError("%s must be [B, S, H, D]" % name)
+    b, s, h, d = t.stride()
+    if d != 1 and t.shape[3] > 1:
+        raise ValueError("%s: the components of a head must be contiguous" % name)
+    return t.data_ptr(), b, s, h
+
+
+def _empty(shape, dtype, device, stream):
+    """A new tensor that belongs to the stream the call is enqueued on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(_torch_stream(device, stream)):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _out_like(t, out, name, stream):
+    """The output tensor of t's shape (new unless given) and its tokens."""
+    if out is None:
+        out = _empty(t.shape, t.dtype, t.device, stream)
+    tokens = _tokens(out, name)
+    if out.shape != t.shape or not _alike(out, t):
+        raise ValueError("%s must be %s in the inputs' dtype and device" % (name, list(t.shape)))
+    return out, tokens
+
+
+def wbmm_rotary_frequencies(sections, base: float = 10000.0, restart: bool = False, device="cuda") -> torch.Tensor:
+    """float32 [P] radians a position for rotary pairs of ``sections`` (pairs
+    of each axis; P their sum): base ** (-i / P) for pair i, or with
+    ``restart`` each axis a ladder of its own, base ** (-j / sections[a])."""
+    if len(sections) == 0 or min(sections) < 0 or sum(sections) < 1 or not base > 0:
+        raise ValueError("sections must be pair counts, base positive")
+    ladders = [n for n in sections if n > 0] if restart else [sum(sections)]
+    f = torch.cat([float(base) ** (-torch.arange(n, dtype=torch.float64) / n) for n in ladders])
+    return f.to(torch.float32).to(device)
+
+
+def _rotary_like(fn_name, x, positions, freqs, sections, adjacent, out, stream):
+    xt = _tokens(x, "input")
+    B, S, H, D = x.shape
+    n = len(sections)
+    if not 1 <= n <= MAX_AXES:
+        raise ValueError("sections must name 1 to %d axes" % MAX_AXES)
+    for t, name in ((positions, "positions"), (freqs, "freqs")):
+        if not isinstance(t, torch.Tensor):
+            raise TypeError("%s must be a torch.Tensor" % name)
+        if t.get_device() != x.get_device():
+            raise ValueError("%s must be on the input's device" % name)
+    if positions.dtype not in (torch.int32, torch.int64):
+        raise TypeError("positions must be int32 or int64")
+    if positions.shape != (n, B, S):
+        raise ValueError("positions must be [axes, B, S] = %s" % [n, B, S])
+    if freqs.dtype != torch.float32:
+        raise TypeError("freqs must be float32")
+    if freqs.shape != (sum(sections),) or not freqs.is_contiguous():
+        raise ValueError("freqs must be contiguous, one value a pair of sections")
+    out, yt = _out_like(x, out, "out", stream)
+    args = _ROTARY_ARGS.pack(*xt, *yt, positions.data_ptr(), positions.element_size(), *positions.stride(),
+                             freqs.data_ptr(), n, *sections, *(0,) * (MAX_AXES - n), 1 if adjacent else 0, B, S, H, D,
+                             _code(x.dtype))
+    _call(fn_name, x.get_device(), args, _stream(x, stream))
+    return out
+
+
+def wbmm_rotary_forward(x, positions, freqs, sections, adjacent: bool = False, out=None, stream=None):
+    """x [B,S,H,D] with the first P pairs of each head turned by their
+    positions: pair i belongs to the axis that ``sections`` (pairs of each
+    axis, P their sum) gives it, and turns by positions[axis,b,s] * freqs[i].
+    Pairs are components (i, i + P), or with ``adjacent`` (2i, 2i + 1).
+    positions: int32 or int64 [axes,B,S]; freqs: float32 [P].  ``out`` may be x
+    itself."""
+    return _rotary_like("wbmm_rotary_forward", x, positions, freqs, sections, adjacent, out, stream)
+
+
+def wbmm_rotary_backward(dy, positions, freqs, sections, adjacent: bool = False, out=None, stream=None):
+    """dx for upstream gradient dy: turned back by the same angles."""
+    return _rotary_like("wbmm_rotary_backward", dy, positions, freqs, sections, adjacent, out, stream)
+
+
+def _attention_sizes(q, k, v, kv_lens, key_mask, scale):
+    """Checks the inputs; returns their tokens, the addresses and strides of
+    lengths and mask, sizes and scale."""
+    qt, kt, vt = _tokens(q, "q"), _tokens(k, "k"), _tokens(v, "v")
+    B, Sq, Hq, D = q.shape
+    Sk, Hk = k.shape[1], k.shape[2]
+    if k.shape != (B, Sk, Hk, D) or v.shape != k.shape:
+        raise ValueError("k and v must be [B, Sk, Hk, D] with q's B and D")
+    if Hk == 0 or Hq % Hk != 0:
+        raise ValueError("q's heads must be a multiple of k's")
+    if not _alike(k, q) or not _alike(v, q):
+        raise ValueError("k and v must match q's dtype and device")
+    lens = mask = mask_b = mask_s = 0
+    if kv_lens is not None:
+        if not isinstance(kv_lens, torch.Tensor) or kv_lens.dtype != torch.int32:
+            raise TypeError("kv_lens must be an int32 tensor")
+        if kv_lens.shape != (B,) or not kv_lens.is_contiguous() or kv_lens.get_device() != q.get_device():
+            raise ValueError("kv_lens must be contiguous [B] on q's device")
+        lens = kv_lens.data_ptr()
+    if key_mask is not None:
+        if not isinstance(key_mask, torch.Tensor) or key_mask.dtype not in (torch.bool, torch.uint8):
+            raise TypeError("key_mask must be a bool or uint8 tensor (true: visible)")
+        if key_mask.shape != (B, Sk) or key_mask.get_device() != q.get_device():
+            raise ValueError("key_mask must be [B, Sk] on q's device")
+        mask = key_mask.data_ptr()
+        mask_b, mask_s = key_mask.stride()
+    scale = D ** -0.5 if scale is None else float(scale)
+    return (*qt, *kt, *vt), (lens, mask, mask_b, mask_s, B, Sq, Sk, Hq, Hk, D, scale, _code(q.dtype))
+
+
+def _attention_call(way, q, pack, stream):
+    """The library call, with a workspace of its own where it needs one:
+    pack(address, bytes) gives the argument struct."""
+    lib = _lib if _lib is not None else load_library()
+    need = getattr(lib, "wbmm_cross_attention_%s_workspace_bytes" % way)(pack(0, 0))
+    # (freed on return, for later work of the same stream)
+    ws = _empty(need, torch.uint8, q.device, stream) if need else None
+    _call("wbmm_cross_attention_" + way, q.get_device(), pack(ws.data_ptr() if need else 0, need), _stream(q, stream))
+
+
+def wbmm_cross_attention_forward(q, k, v, kv_lens=None, key_mask=None, scale=None, need_lse: bool = True, out=None,
+                                 stream=None):
+    """(out, lse) of queries q [B,Sq,Hq,D] that attend to states k, v
+    [B,Sk,Hk,D] (Hk divides Hq: heads in groups): out like q, lse float32
+    [B,Hq,Sq], the logarithm of each query's sum of exponentials (None unless
+    ``need_lse``).  Visible are the first kv_lens[b] states (int32 [B]) that
+    ``key_mask`` [B,Sk] (bool, true: visible) does not hide; a query that sees
+    none gets zeros and minus infinity.  ``scale`` of the scores: D ** -0.5
+    unless given."""
+    tokens, sizes = _attention_sizes(q, k, v, kv_lens, key_mask, scale)
+    out, ot = _out_like(q, out, "out", stream)
+    B, Sq, Hq, _ = q.shape
+    lse = _empty((B, Hq, Sq), torch.float32, q.device, stream) if need_lse else None
+    lse_ptr = lse.data_ptr() if need_lse else 0
+    _attention_call("forward", q, lambda ws, n: _ATTENTION_ARGS.pack(*tokens, *ot, *_NO_TOKENS * 4, lse_ptr, *sizes, ws,
+                                                                     n), stream)
+    return out, lse
+
+
+def wbmm_cross_attention_backward(dout, q, k, v, out, lse, kv_lens=None, key_mask=None, scale=None, dq=None, dk=None,
+                                  dv=None, stream=None):
+    """(dq, dk, dv) for upstream gradient dout, with the forward's inputs and
+    its results out and lse.  Gradients of states that are not visible are
+    zero."""
+    tokens, sizes = _attention_sizes(q, k, v, kv_lens, key_mask, scale)
+    B, Sq, Hq, _ = q.shape
+    ot, gt = _tokens(out, "out"), _tokens(dout, "dout")
+    for t, name in ((out, "out"), (dout, "dout")):
+        if t.shape != q.shape or not _alike(t, q):
+            raise ValueError("%s must match q's shape, dtype and device" % name)
+    _check_tensor(lse, "lse")
+    if lse.dtype != torch.float32 or lse.shape != (B, Hq, Sq) or lse.get_device() != q.get_device():
+        raise ValueError("lse must be float32 [B, Hq, Sq] on q's device")
+    dq, dqt = _out_like(q, dq, "dq", stream)
+    dk, dkt = _out_like(k, dk, "dk", stream)
+    dv, dvt = _out_like(v, dv, "dv", stream)
+    lse_ptr = lse.data_ptr()
+    _attention_call("backward", q, lambda ws, n: _ATTENTION_ARGS.pack(*tokens, *ot, *gt, *dqt, *dkt, *dvt, lse_ptr,
+                                                                      *sizes, ws, n), stream)
+    return dq, dk, dv
+
+
+def _rows(t):
+    """t, or a copy with contiguous components."""
+    return t if t.stride(-1) == 1 or t.shape[-1] <= 1 else t.contiguous()
+
+
+class WBMMRotaryFunction(torch.autograd.Function):
+    """Autograd of the rotary positions (for x; positions and frequencies are
+    constants)."""
+
+    @staticmethod
+    def forward(ctx, x, positions, freqs, sections, adjacent):
+        ctx.sections, ctx.adjacent = tuple(sections), bool(adjacent)
+        ctx.save_for_backward(positions, freqs)
+        return wbmm_rotary_forward(_rows(x), positions, freqs, ctx.sections, ctx.adjacent)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy):
+        positions, freqs = ctx.saved_tensors
+        return wbmm_rotary_backward(_rows(dy), positions, freqs, ctx.sections, ctx.adjacent), None, None, None, None
+
+
+def wbmm_rotary(x, positions, freqs, sections, adjacent: bool = False):
+    """Differentiable rotary positions (see wbmm_rotary_forward)."""
+    return WBMMRotaryFunction.apply(x, positions, freqs, sections, adjacent)
+
+
+class WBMMCrossAttentionFunction(torch.autograd.Function):
+    """Autograd of the cross attention."""
+
+    @staticmethod
+    def forward(ctx, q, k, v, kv_lens, key_mask, scale):
+        q, k, v = _rows(q), _rows(k), _rows(v)
+        out, lse = wbmm_cross_attention_forward(q, k, v, kv_lens, key_mask, scale)
+        ctx.scale = scale
+        ctx.save_for_backward(q, k, v, out, lse, kv_lens, key_mask)
+        return out
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        q, k, v, out, lse, kv_lens, key_mask = ctx.saved_tensors
+        dq, dk, dv = wbmm_cross_attention_backward(_rows(dout), q, k, v, out, lse, kv_lens, key_mask, ctx.scale)
+        return dq, dk, dv, None, None, None
+
+
+def wbmm_cross_attention(q, k, v, kv_lens=None, key_mask=None, scale=None):
+    """Differentiable cross attention (see wbmm_cross_attention_forward)."""
+    return WBMMCrossAttentionFunction.apply(q, k, v, kv_lens, key_mask, scale)

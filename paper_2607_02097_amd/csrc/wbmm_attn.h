@@ -1,0 +1,993 @@
+// Cross attention kernels for gfx950: device code and launchers, instantiated
+// per dtype by wbmm_attn.hip.
+//
+// Per batch entry and key head, row r = s G + g stands for query s of head g
+// of the G query heads that share the key head, so the rows of a group read
+// one set of keys and values:
+//   out_r = sum_j p_rj v_j,  p_rj = exp(scale q_r.k_j - lse_r)
+// over the visible states j (below the sequence's length, not masked).
+//
+// Matrix-core layout
+// ------------------
+// All products run through 32 x 32 tiles (v_mfma_f32_32x32x16_{bf16,f16},
+// 32x32x2_f32).  A lane's result column is l % 32, its 16 result rows are
+// 8 (i / 4) + 4 h + i % 4 with h = l / 32.  Scores are taken transposed,
+// S^T = K Q^T, so a lane holds scores of one query only: maxima and sums run
+// inside the lane and join one partner lane.  The sum over keys of the second
+// product, O^T = V^T P^T, may take the keys in any order as long as both
+// operands agree; with the order in which a lane already holds them, the
+// probabilities are the second operand as they are, without a shuffle.
+// V^T comes from the transposing LDS reads (16-bit) or single-element reads
+// (float32) of the row-major tile.
+//
+// LDS tiles are row-major; 16-byte chunk c of row r sits at slot c ^ swz(r).
+// swz makes both kinds of reads free of bank conflicts: 16 rows at one chunk,
+// and 4 rows at 64 consecutive bytes.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "wbmm_attn_internal.h"
+#include "wbmm_kernels.h"
+
+namespace wbmm {
+
+namespace {
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+
+constexpr float kLog2e = 1.4426950408889634f;
+constexpr float kLn2 = 0.6931471805599453f;
+
+// ------------------------------------------------------------ tile geometry
+
+template <class Tag, int DP>
+struct Tile {
+  static constexpr int ES = Tag::ES;
+  static constexpr int CE = 16 / ES;                              // elements of a chunk
+  static constexpr int PITCH = (DP == 96 ? 128 : DP) * ES;        // bytes of an LDS row
+  static constexpr int LPC = PITCH / 16;                          // chunks of an LDS row
+  static constexpr int NU = DP / (2 * CE);                        // chunk pairs of a row
+  static constexpr int DT = DP / 32;
+  __device__ static int swz(int row) {
+    if constexpr (ES == 2) {
+      if constexpr (PITCH == 256) return ((row & 3) << 2) | ((row >> 2) & 3);
+      if constexpr (PITCH == 128) return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+      return (row >> 2) & 3;
+    } else {
+      if constexpr (PITCH >= 256) return (((row >> 2) & 1) << 3) | (row & 3) | (((row >> 3) & 1) << 2);
+      return (row >> 1) & 7;
+    }
+  }
+  // Row reads: lane l reads chunk 2 u + h of row base + l % 32 (base a
+  // multiple of 32) at rowlane() ^ (u << 5), plus base * PITCH.
+  __device__ static int rowlane(int lane) {
+    const int l31 = lane & 31, h = lane >> 5;
+    return l31 * PITCH + ((h ^ swz(l31)) << 4);
+  }
+  // Column reads, 16-bit: four rows 16 t + 8 g + 4 h + 0..3 of column
+  // 32 dt + l % 32 at (collane() ^ (dt << 6) ^ (g << 5)) + (16 t + 8 g) * PITCH.
+  // float32: row 8 (i / 4) + 4 h + i % 4 of that column at
+  // (collane() ^ colxor32(dt, i)) + (8 (i / 4) + i % 4) * PITCH.
+  __device__ static int collane(int lane) {
+    const int h = lane >> 5;
+    if constexpr (ES == 2) {
+      const int r = (lane >> 2) & 3, q = lane & 3, cg = (lane >> 4) & 1;
+      int slot = cg * 2 + (q >> 1);
+      if constexpr (PITCH == 256) slot ^= r << 2;
+      if constexpr (PITCH == 128) slot ^= ((r >> 1) & 1) << 2;
+      slot ^= h;
+      return (4 * h + r) * PITCH + (slot << 4) + (q & 1) * 8;
+    } else {
+      const int l31 = lane & 31;
+      const int slot = (l31 >> 2) ^ (PITCH >= 256 ? h << 3 : h << 1);
+      return 4 * h * PITCH + (slot << 4) + (l31 & 3) * 4;
+    }
+  }
+  __device__ static constexpr int colxor32(int dt, int i) {
+    if (PITCH >= 256) return (dt << 7) ^ ((i % 4) << 4) ^ (((i / 4) & 1) << 6);
+    return ((((i / 4) & 1) << 2) | ((i % 4) >> 1)) << 4;
+  }
+};
+
+// ----------------------------------------------------------------- products
+
+// acc += A B over one chunk pair (16 or 8 components): chunks of both halves.
+template <class Tag> __device__ inline f32x16 mma_chunk(u32x4 a, u32x4 b, f32x16 c) {
+  if constexpr (Tag::W16) {
+    if constexpr (__is_same(Tag, TagBF16))
+      return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                     0, 0);
+    else
+      return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0,
+                                                    0, 0);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(a[j]), __uint_as_float(b[j]), c, 0, 0,
+                                               0);
+    return c;
+  }
+}
+
+// Result of a 32 x 32 product over the row fragments of an LDS tile (rows
+// base..base+31) with fragments in registers.
+template <class Tag, int DP>
+__device__ inline f32x16 rows_product(const char *tile, int rowlane, int base, const u32x4 *b) {
+  using T = Tile<Tag, DP>;
+  f32x16 acc = {};
+#pragma unroll
+  for (int u = 0; u < T::NU; ++u) {
+    const u32x4 a = *(const u32x4 *)(tile + (rowlane ^ (u << 5)) + base * T::PITCH);
+    acc = mma_chunk<Tag>(a, b[u], acc);
+  }
+  return acc;
+}
+
+// Second operand over 32 rows made of a lane's 16 results.
+template <class Tag> struct Weights { u32x4 w[2]; };
+template <> struct Weights<TagF32> { f32x16 w; };
+template <class Tag> __device__ inline Weights<Tag> to_weights(const f32x16 &p) {
+  Weights<Tag> r;
+  if constexpr (Tag::W16) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) r.w[t][j] = pack2<Tag>(p[8 * t + 2 * j], p[8 * t + 2 * j + 1]);
+  } else {
+    r.w = p;
+  }
+  return r;
+}
+
+// acc[dt] += (columns of the LDS tile's rows base..base+31)^T weights.
+template <class Tag, int DP>
+__device__ inline void cols_product(const char *tile, int collane, int base, const Weights<Tag> &p, f32x16 *acc) {
+  using T = Tile<Tag, DP>;
+  if constexpr (Tag::W16) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int dt = 0; dt < T::DT; ++dt) {
+        s16x4 v[2];
+#pragma unroll
+        for (int g = 0; g < 2; ++g)
+          v[g] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+              (lds_s16x4 *)(tile + (collane ^ (dt << 6) ^ (g << 5)) + (base + 16 * t + 8 * g) * T::PITCH));
+        const u32x2 lo = __builtin_bit_cast(u32x2, v[0]), hi = __builtin_bit_cast(u32x2, v[1]);
+        const u32x4 a = {lo[0], lo[1], hi[0], hi[1]};
+        acc[dt] = mma_chunk<Tag>(a, p.w[t], acc[dt]);
+      }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+      for (int dt = 0; dt < T::DT; ++dt) {
+        const float a =
+            *(const float *)(tile + (collane ^ T::colxor32(dt, i)) + (base + 8 * (i / 4) + i % 4) * T::PITCH);
+        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p.w[i], acc[dt], 0, 0, 0);
+      }
+  }
+}
+
+// ------------------------------------------------------------------- memory
+
+// Chunk (16 bytes from component d0 on) of a row of D components; what lies
+// past D is zero.  VEC: rows are whole 16-byte pieces.
+template <class Tag>
+__device__ inline u32x4 load_chunk(const char *row, int d0, int D, int vec) {
+  u32x4 v = {0, 0, 0, 0};
+  if (d0 >= D) return v;
+  if (vec) return *(const u32x4 *)(row + d0 * Tag::ES);
+  if constexpr (Tag::W16) {
+    const u16 *p = (const u16 *)row + d0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (d0 + j < D) v[j / 2] |= (uint32_t)p[j] << (16 * (j & 1));
+  } else {
+    const uint32_t *p = (const uint32_t *)row + d0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (d0 + j < D) v[j] = p[j];
+  }
+  return v;
+}
+
+// Four consecutive components of a row, rounded once, stored from d0 on.
+template <class Tag>
+__device__ inline void store4(char *row, int d0, int D, int vec, float a, float b, float c, float d) {
+  if (d0 >= D) return;
+  const float f[4] = {a, b, c, d};
+  if constexpr (Tag::W16) {
+    const uint32_t lo = pack2<Tag>(a, b), hi = pack2<Tag>(c, d);
+    if (vec) {
+      *(u32x2 *)(row + d0 * 2) = (u32x2){lo, hi};
+    } else {
+      const u16 e[4] = {(u16)lo, (u16)(lo >> 16), (u16)hi, (u16)(hi >> 16)};
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (d0 + j < D) ((u16 *)row)[d0 + j] = e[j];
+    }
+  } else if (vec) {
+    *(f32x4 *)(row + d0 * 4) = (f32x4){a, b, c, d};
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (d0 + j < D) ((float *)row)[d0 + j] = f[j];
+  }
+}
+
+// A tile of ROWS rows on its way from memory to LDS through registers.
+template <class Tag, int DP, int ROWS, int THREADS>
+struct Mover {
+  using T = Tile<Tag, DP>;
+  static constexpr int RPP = THREADS / T::LPC;  // rows a pass
+  static constexpr int NP = (ROWS + RPP - 1) / RPP;
+  u32x4 r[NP];
+  __device__ static int chunk(int tid) { return tid % T::LPC; }
+  __device__ static int row(int tid, int p) { return tid / T::LPC + p * RPP; }
+  __device__ void store(char *tile, int tid) const {
+#pragma unroll
+    for (int p = 0; p < NP; ++p) {
+      const int rw = row(tid, p);
+      if (ROWS % RPP == 0 || rw < ROWS)
+        *(u32x4 *)(tile + rw * T::PITCH + ((chunk(tid) ^ T::swz(rw)) << 4)) = r[p];
+    }
+  }
+};
+
+// Rows first .. first + ROWS - 1 of the states of one head: those from `end`
+// on, and masked ones, as zeros (what lies there may be anything).
+template <class Tag, int DP, int ROWS, int THREADS>
+struct StateMover : Mover<Tag, DP, ROWS, THREADS> {
+  using M = Mover<Tag, DP, ROWS, THREADS>;
+  __device__ void load(const char *base, int64_t stride, int first, int end, const uint8_t *mask, int64_t mask_s, int D,
+                       int vec, int tid) {
+    const int d0 = M::chunk(tid) * M::T::CE;
+#pragma unroll
+    for (int p = 0; p < M::NP; ++p) {
+      const int j = first + M::row(tid, p);
+      u32x4 v = {0, 0, 0, 0};
+      if (j < end && (ROWS % M::RPP == 0 || M::row(tid, p) < ROWS)) {
+        v = load_chunk<Tag>(base + j * stride, d0, D, vec);
+        if (mask && !mask[j * mask_s]) v = (u32x4){0, 0, 0, 0};
+      }
+      this->r[p] = v;
+    }
+  }
+};
+
+__device__ inline float other_half_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false,
+                                                  false);
+  return fmaxf(__builtin_bit_cast(float, (uint32_t)r[0]), __builtin_bit_cast(float, (uint32_t)r[1]));
+}
+__device__ inline float other_half_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false,
+                                                  false);
+  return __builtin_bit_cast(float, (uint32_t)r[0]) + __builtin_bit_cast(float, (uint32_t)r[1]);
+}
+__device__ inline float exp2_(float v) { return __builtin_amdgcn_exp2f(v); }
+
+// Visibility of states first .. first + n - 1, bit by bit, alike in all lanes.
+__device__ inline uint64_t visible(const AttnArgs &a, int64_t b, int first, int n, int end, int lane) {
+  const int j = first + lane;
+  bool see = lane < n && j < end;
+  if (a.mask && see) see = a.mask[b * a.mask_b + j * a.mask_s] != 0;
+  return __ballot(see);
+}
+
+// Workgroup `id` of `n` onto a unit of work such that each die (workgroups
+// are dealt to the eight in turn) takes one run of consecutive units, which
+// share keys and values in its L2.
+__device__ inline int64_t unit_of(int64_t id, int64_t n) {
+  const int64_t per = n >> 3, rem = n & 7, die = id & 7, slot = id >> 3;
+  return die * per + (die < rem ? die : rem) + slot;
+}
+
+__device__ inline int length_of(const AttnArgs &a, int64_t b) {
+  int len = a.Sk;
+  if (a.lens) {
+    len = a.lens[b];
+    len = len < 0 ? 0 : len > a.Sk ? a.Sk : len;
+  }
+  return len;
+}
+
+// Row fragments of 32 rows of a group (second operand): lane l has chunks
+// 2 u + h of row r (nothing for r >= R).
+template <class Tag, int DP>
+__device__ inline void load_rows(const AttnArgs &a, const Tokens &t, int64_t b, int hk, int r, int lane, u32x4 *f) {
+  using T = Tile<Tag, DP>;
+  const int h = lane >> 5;
+  if (r < a.R) {
+    const int s = r / a.G, g = r - s * a.G;
+    const char *row = t.p + b * t.b + s * t.s + (int64_t)(hk * a.G + g) * t.h;
+#pragma unroll
+    for (int u = 0; u < T::NU; ++u) f[u] = load_chunk<Tag>(row, (2 * u + h) * T::CE, a.D, a.vec);
+  } else {
+#pragma unroll
+    for (int u = 0; u < T::NU; ++u) f[u] = (u32x4){0, 0, 0, 0};
+  }
+}
+
+// Scores of 32 states (one lane: 16 of one query) to weights: running maximum
+// `top` (in log2 units, with lag) and the lane's part of the sum.  Returns
+// through `scale` what the earlier results have to be multiplied by where any
+// lane's maximum moved.
+constexpr float kLag = 8.f;
+
+template <int NB>
+__device__ inline bool running_top(const f32x16 *s, float c, float *top, float *fix) {
+  float m = s[0][0];
+#pragma unroll
+  for (int k = 0; k < NB; ++k)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) m = fmaxf(m, s[k][i]);
+  m = other_half_max(m) * c;
+  // The maximum may lag by up to kLag: weights then reach 2^kLag, which costs
+  // no precision in floating point, and nearly all tiles skip the rescaling.
+  const bool move = m > *top + kLag;
+  if (!__any(move)) return false;
+  const float t = fmaxf(*top, m);
+  *fix = t == -INFINITY ? 1.f : exp2_(*top - t);
+  *top = t;
+  return true;
+}
+
+// ------------------------------------------------------------------ forward
+
+// A workgroup takes 32 (4 / WK) rows and runs over its part of the states in
+// tiles of BN, double-buffered in LDS, the next tile on its way in registers.
+// WK waves share 32 rows and split each tile's states, joined at the end.
+template <class Tag, int DP, int WK>
+struct FwdShape {
+  static constexpr int WR = 4 / WK;
+  static constexpr int BM = 32 * WR;
+  static constexpr int KW = Tag::W16 && WK == 1 ? 64 : 32;  // states of a wave per tile
+  static constexpr int BN = KW * WK;
+  static constexpr int NB = KW / 32;
+  static constexpr int TILE = BN * Tile<Tag, DP>::PITCH;
+  static constexpr int LDS = 4 * TILE;
+};
+
+template <class Tag, int DP, int WK>
+__global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
+  using T = Tile<Tag, DP>;
+  using F = FwdShape<Tag, DP, WK>;
+  constexpr int NB = F::NB, DT = T::DT;
+  extern __shared__ __align__(512) char attn_smem[];
+  char *const smem = attn_smem;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wr = wave % F::WR, wk = wave / F::WR, h = lane >> 5;
+  const int tiles = (a.R + F::BM - 1) / F::BM;
+  int64_t unit = unit_of(blockIdx.x, gridDim.x);
+  const int rt = (int)(unit % tiles);
+  unit /= tiles;
+  const int split = (int)(unit % a.splits);
+  const int64_t bh = unit / a.splits;
+  const int64_t b = bh / a.Hk;
+  const int hk = (int)(bh - b * a.Hk);
+  const int len = length_of(a, b);
+  const int all = (len + F::BN - 1) / F::BN;
+  const int t0 = (int)((int64_t)all * split / a.splits), t1 = (int)((int64_t)all * (split + 1) / a.splits);
+  const int r = rt * F::BM + wr * 32 + (lane & 31);
+
+  u32x4 qf[T::NU];
+  load_rows<Tag, DP>(a, a.q, b, hk, r, lane, qf);
+  const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
+  const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
+  StateMover<Tag, DP, F::BN, 256> mk, mv;
+  const int rowlane = T::rowlane(lane), collane = T::collane(lane);
+
+  f32x16 acc[DT] = {};
+  float top = -INFINITY, sum = 0.f;
+  if (t0 < t1) {
+    mk.load(kb, a.k.s, t0 * F::BN, len, mask, a.mask_s, a.D, a.vec, tid);
+    mv.load(vb, a.v.s, t0 * F::BN, len, mask, a.mask_s, a.D, a.vec, tid);
+  }
+  for (int t = t0; t < t1; ++t) {
+    char *kt = smem + (t & 1) * 2 * F::TILE, *vt = kt + F::TILE;
+    mk.store(kt, tid);
+    mv.store(vt, tid);
+    __syncthreads();
+    if (t + 1 < t1) {
+      mk.load(kb, a.k.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, a.vec, tid);
+      mv.load(vb, a.v.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, a.vec, tid);
+    }
+    f32x16 s[NB];
+#pragma unroll
+    for (int k = 0; k < NB; ++k) s[k] = rows_product<Tag, DP>(kt, rowlane, wk * F::KW + 32 * k, qf);
+    if (a.mask || (t + 1) * F::BN > len) {
+      constexpr uint64_t FULL = F::KW == 64 ? ~(uint64_t)0 : 0xffffffffu;
+      const uint64_t see = (visible(a, b, t * F::BN, F::BN, len, lane) >> (wk * F::KW)) & FULL;
+      if (see != FULL) {
+#pragma unroll
+        for (int k = 0; k < NB; ++k) {
+          const uint32_t bits = (uint32_t)(see >> (32 * k)) >> (4 * h);
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (!((bits >> (8 * (i / 4) + i % 4)) & 1)) s[k][i] = -INFINITY;
+        }
+      }
+    }
+    float fix;
+    if (running_top<NB>(s, a.c, &top, &fix)) {
+      sum *= fix;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) acc[d] *= fix;
+    }
+    const float sub = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      float part[2] = {0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[k][i] = exp2_(__builtin_fmaf(s[k][i], a.c, -sub));
+        part[i & 1] += s[k][i];
+      }
+      sum += part[0] + part[1];
+      // Weights are rounded to the inputs' type for the second product; their
+      // sum is taken before that, in float32.
+      const Weights<Tag> w = to_weights<Tag>(s[k]);
+      cols_product<Tag, DP>(vt, collane, wk * F::KW + 32 * k, w, acc);
+    }
+  }
+  sum = other_half_sum(sum);
+
+  if constexpr (WK > 1) {
+    // join the waves that share rows
+    float *xo = (float *)smem;  // [wave][16 DT][64], then top and sum
+    constexpr int PER = (16 * DT + 2) * 64;
+    static_assert((4 - F::WR) * PER * 4 <= F::LDS, "the waves' results fit the tiles' space");
+    __syncthreads();
+    if (wk > 0) {
+      float *o = xo + (wave - F::WR) * PER + lane;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[(d * 16 + i) * 64] = acc[d][i];
+      o[16 * DT * 64] = top;
+      o[(16 * DT + 1) * 64] = sum;
+    }
+    __syncthreads();
+    if (wk > 0) return;
+    for (int w = 1; w < WK; ++w) {
+      const float *o = xo + (wave + (w - 1) * F::WR) * PER + lane;
+      const float top2 = o[16 * DT * 64], sum2 = o[(16 * DT + 1) * 64];
+      const float t = fmaxf(top, top2);
+      const float f1 = top == t ? 1.f : exp2_(top - t), f2 = top2 == t ? 1.f : exp2_(top2 - t);
+      sum = sum * f1 + sum2 * f2;
+      top = t;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] = acc[d][i] * f1 + o[(d * 16 + i) * 64] * f2;
+    }
+  }
+  if (r >= a.R) return;
+  // a row that sees nothing: zeros, and minus infinity
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  const float lse2 = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
+  if (a.splits > 1) {
+    const int64_t at = (split * a.B * a.Hk + bh) * a.R + r;
+    if (h == 0) a.part_l[at] = lse2;
+    float *o = a.part_o + at * a.D;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        store4<TagF32>((char *)o, 32 * d + 8 * (i / 4) + 4 * h, a.D, a.D % 4 == 0, acc[d][i] * inv, acc[d][i + 1] * inv,
+                       acc[d][i + 2] * inv, acc[d][i + 3] * inv);
+    return;
+  }
+  const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
+  if (a.lse && h == 0) a.lse[(b * a.Hq + hq) * a.Sq + sq] = lse2 * kLn2;
+  char *o = a.o.p + b * a.o.b + sq * a.o.s + hq * a.o.h;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+      store4<Tag>(o, 32 * d + 8 * (i / 4) + 4 * h, a.D, a.vec, acc[d][i] * inv, acc[d][i + 1] * inv, acc[d][i + 2] * inv,
+                  acc[d][i + 3] * inv);
+}
+
+// ------------------------------------------------- forward, a handful of rows
+
+// At most 32 rows a key head (single tokens, drafts): the states are read
+// once and bound the kernel.  Each wave runs over blocks of 32 states of its
+// own; keys go from memory straight into the product's first operand, values
+// through a piece of LDS that only this wave uses, so no barrier is needed.
+template <class Tag, int DP>
+__global__ __launch_bounds__(256, 2) void attn_token_kernel(AttnArgs a) {
+  using T = Tile<Tag, DP>;
+  constexpr int DT = T::DT, TILE = 32 * T::PITCH;
+  extern __shared__ __align__(512) char attn_smem[];
+  char *const smem = attn_smem;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h = lane >> 5, l31 = lane & 31;
+  int64_t unit = unit_of(blockIdx.x, gridDim.x);
+  const int split = (int)(unit % a.splits);
+  const int64_t bh = unit / a.splits;
+  const int64_t b = bh / a.Hk;
+  const int hk = (int)(bh - b * a.Hk);
+  const int len = length_of(a, b);
+  const int all = (len + 31) / 32;
+  const int t0 = (int)((int64_t)all * split / a.splits), t1 = (int)((int64_t)all * (split + 1) / a.splits);
+
+  u32x4 qf[T::NU], kf[T::NU];
+  load_rows<Tag, DP>(a, a.q, b, hk, l31, lane, qf);
+  const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
+  const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
+  StateMover<Tag, DP, 32, 64> mv;
+  char *vt = smem + wave * TILE;
+  const int collane = T::collane(lane);
+  f32x16 acc[DT] = {};
+  float top = -INFINITY, sum = 0.f;
+  int t = t0 + wave;
+  auto load_k = [&](int blk) {
+    const int j = blk * 32 + l31;
+    bool see = j < len;
+    if (mask && see) see = mask[j * a.mask_s] != 0;
+#pragma unroll
+    for (int u = 0; u < T::NU; ++u)
+      kf[u] = see ? load_chunk<Tag>(kb + j * a.k.s, (2 * u + h) * T::CE, a.D, a.vec) : (u32x4){0, 0, 0, 0};
+  };
+  if (t < t1) {
+    load_k(t);
+    mv.load(vb, a.v.s, t * 32, len, mask, a.mask_s, a.D, a.vec, lane);
+  }
+  for (; t < t1; t += 4) {
+    f32x16 s = {};
+#pragma unroll
+    for (int u = 0; u < T::NU; ++u) s = mma_chunk<Tag>(kf[u], qf[u], s);
+    if (t + 4 < t1) load_k(t + 4);
+    mv.store(vt, lane);
+    if (t + 4 < t1) mv.load(vb, a.v.s, (t + 4) * 32, len, mask, a.mask_s, a.D, a.vec, lane);
+    if (a.mask || (t + 1) * 32 > len) {
+      const uint32_t bits = (uint32_t)visible(a, b, t * 32, 32, len, lane) >> (4 * h);
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        if (!((bits >> (8 * (i / 4) + i % 4)) & 1)) s[i] = -INFINITY;
+    }
+    float fix;
+    if (running_top<1>(&s, a.c, &top, &fix)) {
+      sum *= fix;
+#pragma unroll
+      for (int d = 0; d < DT; ++d) acc[d] *= fix;
+    }
+    const float sub = top == -INFINITY ? 0.f : top;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[i] = exp2_(__builtin_fmaf(s[i], a.c, -sub));
+      sum += s[i];
+    }
+    // this wave's writes to LDS come before its own reads
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    const Weights<Tag> w = to_weights<Tag>(s);
+    cols_product<Tag, DP>(vt, collane, 0, w, acc);
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  }
+  sum = other_half_sum(sum);
+
+  // join the four waves: [wave][row][DP + 4] results, then each wave's top
+  // and sum per row
+  constexpr int OP = DP + 4;
+  float *xo = (float *)smem, *xt = xo + 4 * 32 * OP, *xs = xt + 128;
+  __syncthreads();
+  if (l31 < a.R) {
+    float *o = xo + (wave * 32 + l31) * OP;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *(f32x4 *)(o + 32 * d + 8 * (i / 4) + 4 * h) = (f32x4){acc[d][i], acc[d][i + 1], acc[d][i + 2], acc[d][i + 3]};
+    if (h == 0) {
+      xt[wave * 32 + l31] = top;
+      xs[wave * 32 + l31] = sum;
+    }
+  }
+  __syncthreads();
+  for (int e = tid; e < a.R * DP; e += 256) {
+    const int r = e / DP, d = e % DP;
+    float t4 = -INFINITY, s4 = 0.f, o4 = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) t4 = fmaxf(t4, xt[w * 32 + r]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float tw = xt[w * 32 + r];
+      const float f = tw == t4 ? 1.f : exp2_(tw - t4);
+      s4 += xs[w * 32 + r] * f;
+      o4 += xo[(w * 32 + r) * OP + d] * f;
+    }
+    if (d >= a.D) continue;
+    const float inv = s4 == 0.f ? 0.f : 1.f / s4;
+    const float lse2 = s4 == 0.f ? -INFINITY : t4 + __builtin_amdgcn_logf(s4);
+    if (a.splits > 1) {
+      const int64_t at = (split * a.B * a.Hk + bh) * a.R + r;
+      a.part_o[at * a.D + d] = o4 * inv;
+      if (d == 0) a.part_l[at] = lse2;
+    } else {
+      const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
+      char *o = a.o.p + b * a.o.b + sq * a.o.s + hq * a.o.h;
+      if constexpr (Tag::W16)
+        ((u16 *)o)[d] = (u16)pack2<Tag>(o4 * inv, 0.f);
+      else
+        ((float *)o)[d] = o4 * inv;
+      if (a.lse && d == 0) a.lse[(b * a.Hq + hq) * a.Sq + sq] = lse2 * kLn2;
+    }
+  }
+}
+
+// Joins the partial results of the splits, weighted by their shares of the
+// sum, in their order.  A thread takes one component of one row.
+template <class Tag>
+__global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
+  const int64_t n = a.B * a.Hk * (int64_t)a.R;
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (e >= n * a.D) return;
+  const int64_t row = e / a.D;
+  const int d = (int)(e - row * a.D);
+  float top = -INFINITY;
+  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_l[s * n + row]);
+  float sum = 0.f, o = 0.f;
+  for (int s = 0; s < a.splits; ++s) {
+    const float l = a.part_l[s * n + row];
+    const float w = top == -INFINITY ? (l != l ? l : 0.f) : exp2_(l - top);
+    sum += w;
+    o += w * a.part_o[(s * n + row) * a.D + d];
+  }
+  o = sum == 0.f ? 0.f : o / sum;
+  const int64_t bh = row / a.R, b = bh / a.Hk;
+  const int r = (int)(row - bh * a.R), hk = (int)(bh - b * a.Hk);
+  const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
+  char *p = a.o.p + b * a.o.b + sq * a.o.s + hq * a.o.h;
+  if constexpr (Tag::W16)
+    ((u16 *)p)[d] = (u16)pack2<Tag>(o, 0.f);
+  else
+    ((float *)p)[d] = o;
+  if (a.lse && d == 0)
+    a.lse[(b * a.Hq + hq) * a.Sq + sq] = (sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum)) * kLn2;
+}
+
+// ----------------------------------------------------------------- backward
+//
+// With p recomputed from the forward's lse, delta_r = do_r.o_r and
+// ds = p (do.v - delta):  dq = scale ds K,  dk = scale ds^T Q,  dv = p^T do.
+// Two kernels recompute the scores, one per owner of the results (rows for
+// dq, states for dk and dv), so every sum has one owner and a fixed order: no
+// atomics, and the same bits every time.
+
+// Per row {lse in log2 units, delta}; rows that see nothing get +infinity, so
+// that every weight comes out as zero.  Sixteen lanes a row.
+template <class Tag>
+__global__ __launch_bounds__(256) void attn_rowstat_kernel(AttnArgs a) {
+  constexpr int CE = 16 / Tag::ES;
+  const int64_t n = a.B * a.Hk * (int64_t)a.R;
+  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const int l = threadIdx.x & 15;
+  float d = 0.f;
+  const int64_t at = row < n ? row : n - 1;
+  const int64_t bh = at / a.R, b = bh / a.Hk;
+  const int r = (int)(at - bh * a.R), hk = (int)(bh - b * a.Hk);
+  const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
+  const char *o = a.o.p + b * a.o.b + sq * a.o.s + hq * a.o.h;
+  const char *g = a.dout.p + b * a.dout.b + sq * a.dout.s + hq * a.dout.h;
+  for (int c = l * CE; c < a.D; c += 16 * CE) {
+    const u32x4 x = load_chunk<Tag>(o, c, a.D, a.vec), y = load_chunk<Tag>(g, c, a.D, a.vec);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if constexpr (Tag::W16) {
+        d += to_f32<Tag>((u16)(x[j] & 0xffff)) * to_f32<Tag>((u16)(y[j] & 0xffff));
+        d += to_f32<Tag>((u16)(x[j] >> 16)) * to_f32<Tag>((u16)(y[j] >> 16));
+      } else {
+        d += __uint_as_float(x[j]) * __uint_as_float(y[j]);
+      }
+    }
+  }
+#pragma unroll
+  for (int m = 8; m; m >>= 1) d += __shfl_xor(d, m, 16);
+  if (l == 0 && row < n) {
+    const float lse = a.lse[(b * a.Hq + hq) * a.Sq + sq];
+    a.rowstat[row] = lse == -INFINITY ? make_float2(INFINITY, 0.f) : make_float2(lse * kLog2e, d);
+  }
+}
+
+// dq: as the forward, a workgroup takes 128 rows and runs over all states.
+template <class Tag, int DP>
+struct DqShape {
+  static constexpr int BN = Tag::W16 ? 64 : 32;
+  static constexpr int TILE = BN * Tile<Tag, DP>::PITCH;
+  static constexpr int LDS = 4 * TILE;
+};
+
+template <class Tag, int DP>
+__global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs a) {
+  using T = Tile<Tag, DP>;
+  using F = DqShape<Tag, DP>;
+  constexpr int DT = T::DT, NB = F::BN / 32;
+  extern __shared__ __align__(512) char attn_smem[];
+  char *const smem = attn_smem;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
+  const int tiles = (a.R + 127) / 128;
+  const int64_t unit = unit_of(blockIdx.x, gridDim.x), bh = unit / tiles, b = bh / a.Hk;
+  const int rt = (int)(unit - bh * tiles), hk = (int)(bh - b * a.Hk);
+  const int len = length_of(a, b);
+  const int t1 = (len + F::BN - 1) / F::BN;
+  const int r = rt * 128 + wave * 32 + (lane & 31);
+  u32x4 qf[T::NU], gf[T::NU];
+  load_rows<Tag, DP>(a, a.q, b, hk, r, lane, qf);
+  load_rows<Tag, DP>(a, a.dout, b, hk, r, lane, gf);
+  float2 st = make_float2(INFINITY, 0.f);
+  if (r < a.R) st = a.rowstat[bh * a.R + r];
+  const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
+  const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
+  StateMover<Tag, DP, F::BN, 256> mk, mv;
+  const int rowlane = T::rowlane(lane), collane = T::collane(lane);
+  f32x16 acc[DT] = {};
+  if (t1 > 0) {
+    mk.load(kb, a.k.s, 0, len, mask, a.mask_s, a.D, a.vec, tid);
+    mv.load(vb, a.v.s, 0, len, mask, a.mask_s, a.D, a.vec, tid);
+  }
+  for (int t = 0; t < t1; ++t) {
+    char *kt = smem + (t & 1) * 2 * F::TILE, *vt = kt + F::TILE;
+    mk.store(kt, tid);
+    mv.store(vt, tid);
+    __syncthreads();
+    if (t + 1 < t1) {
+      mk.load(kb, a.k.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, a.vec, tid);
+      mv.load(vb, a.v.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, a.vec, tid);
+    }
+    uint64_t see = ~(uint64_t)0;
+    if (a.mask || (t + 1) * F::BN > len) see = visible(a, b, t * F::BN, F::BN, len, lane);
+#pragma unroll
+    for (int k = 0; k < NB; ++k) {
+      f32x16 s = rows_product<Tag, DP>(kt, rowlane, 32 * k, qf);
+      const f32x16 dp = rows_product<Tag, DP>(vt, rowlane, 32 * k, gf);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = exp2_(__builtin_fmaf(s[i], a.c, -st.x)) * (dp[i] - st.y);
+      const uint32_t seen = (uint32_t)(see >> (32 * k));
+      if (seen != 0xffffffffu) {
+        const uint32_t bits = seen >> (4 * h);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (!((bits >> (8 * (i / 4) + i % 4)) & 1)) s[i] = 0.f;
+      }
+      // ds is rounded to the inputs' type for its product
+      const Weights<Tag> w = to_weights<Tag>(s);
+      cols_product<Tag, DP>(kt, collane, 32 * k, w, acc);
+    }
+  }
+  if (r >= a.R) return;
+  const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
+  char *o = a.dq.p + b * a.dq.b + sq * a.dq.s + hq * a.dq.h;
+  const float f = a.scale;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4)
+      store4<Tag>(o, 32 * d + 8 * (i / 4) + 4 * h, a.D, a.vec, acc[d][i] * f, acc[d][i + 1] * f, acc[d][i + 2] * f,
+                  acc[d][i + 3] * f);
+}
+
+// dk, dv: a workgroup takes 128 states, 32 a wave, and runs over the rows of
+// the key head (or its part of them) in tiles of 32.  Scores are taken as
+// S = Q K^T here, so a lane holds weights of one state and they are the second
+// operand of dv^T = do^T p and dk^T = q^T ds as they are.
+template <class Tag, int DP>
+struct DkvShape {
+  static constexpr int BR = 32;
+  static constexpr int TILE = BR * Tile<Tag, DP>::PITCH;
+  static constexpr int STAT = 4 * TILE;  // two row statistics tiles behind the tiles
+  static constexpr int LDS = STAT + 2 * 2 * BR * 4;
+};
+
+// Rows first .. first + ROWS - 1 of a group.
+template <class Tag, int DP, int ROWS>
+struct RowMover : Mover<Tag, DP, ROWS, 256> {
+  using M = Mover<Tag, DP, ROWS, 256>;
+  __device__ void load(const AttnArgs &a, const Tokens &t, int64_t b, int hk, int first, int end, int tid) {
+    const int d0 = M::chunk(tid) * M::T::CE;
+#pragma unroll
+    for (int p = 0; p < M::NP; ++p) {
+      const int r = first + M::row(tid, p);
+      this->r[p] = (u32x4){0, 0, 0, 0};
+      if (r < end && (ROWS % M::RPP == 0 || M::row(tid, p) < ROWS)) {
+        const int s = r / a.G, g = r - s * a.G;
+        this->r[p] = load_chunk<Tag>(t.p + b * t.b + s * t.s + (int64_t)(hk * a.G + g) * t.h, d0, a.D, a.vec);
+      }
+    }
+  }
+};
+
+template <class Tag, int DP>
+__global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnArgs a) {
+  using T = Tile<Tag, DP>;
+  using F = DkvShape<Tag, DP>;
+  constexpr int DT = T::DT;
+  extern __shared__ __align__(512) char attn_smem[];
+  char *const smem = attn_smem;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h = lane >> 5, l31 = lane & 31;
+  const int tiles = (a.Sk + 127) / 128;
+  int64_t unit = unit_of(blockIdx.x, gridDim.x);
+  const int kt0 = (int)(unit % tiles);
+  unit /= tiles;
+  const int part = (int)(unit % a.row_parts);
+  const int64_t bh = unit / a.row_parts, b = bh / a.Hk;
+  const int hk = (int)(bh - b * a.Hk);
+  const int len = length_of(a, b);
+  const int j = kt0 * 128 + wave * 32 + l31;
+  const int all = (a.R + F::BR - 1) / F::BR;
+  const int t0 = (int)((int64_t)all * part / a.row_parts);
+  int t1 = (int)((int64_t)all * (part + 1) / a.row_parts);
+  if (kt0 * 128 >= len) t1 = t0;  // no state of the tile is visible
+
+  bool see = j < len;
+  if (a.mask && see) see = a.mask[b * a.mask_b + j * a.mask_s] != 0;
+  u32x4 kf[T::NU], vf[T::NU];
+  {
+    const char *kr = a.k.p + b * a.k.b + hk * a.k.h + j * a.k.s, *vr = a.v.p + b * a.v.b + hk * a.v.h + j * a.v.s;
+#pragma unroll
+    for (int u = 0; u < T::NU; ++u) {
+      const int d0 = (2 * u + h) * T::CE;
+      kf[u] = see ? load_chunk<Tag>(kr, d0, a.D, a.vec) : (u32x4){0, 0, 0, 0};
+      vf[u] = see ? load_chunk<Tag>(vr, d0, a.D, a.vec) : (u32x4){0, 0, 0, 0};
+    }
+  }
+  RowMover<Tag, DP, F::BR> mq, mg;
+  float2 st = make_float2(INFINITY, 0.f);
+  auto load = [&](int t) {
+    mq.load(a, a.q, b, hk, t * F::BR, a.R, tid);
+    mg.load(a, a.dout, b, hk, t * F::BR, a.R, tid);
+    if (tid < F::BR) st = t * F::BR + tid < a.R ? a.rowstat[bh * a.R + t * F::BR + tid] : make_float2(INFINITY, 0.f);
+  };
+  const int rowlane = T::rowlane(lane), collane = T::collane(lane);
+  f32x16 dk[DT] = {}, dv[DT] = {};
+  if (t0 < t1) load(t0);
+  for (int t = t0; t < t1; ++t) {
+    char *qt = smem + (t & 1) * 2 * F::TILE, *gt = qt + F::TILE;
+    float *stat = (float *)(smem + F::STAT) + (t & 1) * 2 * F::BR;
+    mq.store(qt, tid);
+    mg.store(gt, tid);
+    if (tid < F::BR) {
+      stat[tid] = st.x;
+      stat[F::BR + tid] = st.y;
+    }
+    __syncthreads();
+    if (t + 1 < t1) load(t + 1);
+    f32x16 s = rows_product<Tag, DP>(qt, rowlane, 0, kf);
+    f32x16 dp = rows_product<Tag, DP>(gt, rowlane, 0, vf);
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const f32x4 l4 = *(const f32x4 *)(stat + 2 * i + 4 * h);
+      const f32x4 d4 = *(const f32x4 *)(stat + F::BR + 2 * i + 4 * h);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[i + e] = exp2_(__builtin_fmaf(s[i + e], a.c, -l4[e]));
+        dp[i + e] = s[i + e] * (dp[i + e] - d4[e]);
+      }
+    }
+    // p and ds are rounded to the inputs' type for their products
+    const Weights<Tag> wp = to_weights<Tag>(s);
+    cols_product<Tag, DP>(gt, collane, 0, wp, dv);
+    const Weights<Tag> wd = to_weights<Tag>(dp);
+    cols_product<Tag, DP>(qt, collane, 0, wd, dk);
+  }
+  if (j >= a.Sk) return;
+  // a state that is not visible has its column of results to itself: zeros
+  const float fk = a.scale;
+  if (a.row_parts > 1) {
+    const int64_t at = ((part * a.B * a.Hk + bh) * a.Sk + j) * a.D;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) {
+        const int d0 = 32 * d + 8 * (i / 4) + 4 * h, vec = a.D % 4 == 0;
+        store4<TagF32>((char *)(a.part_dk + at), d0, a.D, vec, dk[d][i] * fk, dk[d][i + 1] * fk, dk[d][i + 2] * fk,
+                       dk[d][i + 3] * fk);
+        store4<TagF32>((char *)(a.part_dv + at), d0, a.D, vec, dv[d][i], dv[d][i + 1], dv[d][i + 2], dv[d][i + 3]);
+      }
+    return;
+  }
+  char *ok = a.dk.p + b * a.dk.b + j * a.dk.s + hk * a.dk.h, *ov = a.dv.p + b * a.dv.b + j * a.dv.s + hk * a.dv.h;
+#pragma unroll
+  for (int d = 0; d < DT; ++d)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const int d0 = 32 * d + 8 * (i / 4) + 4 * h;
+      if (!see) {
+        store4<Tag>(ok, d0, a.D, a.vec, 0.f, 0.f, 0.f, 0.f);
+        store4<Tag>(ov, d0, a.D, a.vec, 0.f, 0.f, 0.f, 0.f);
+        continue;
+      }
+      store4<Tag>(ok, d0, a.D, a.vec, dk[d][i] * fk, dk[d][i + 1] * fk, dk[d][i + 2] * fk, dk[d][i + 3] * fk);
+      store4<Tag>(ov, d0, a.D, a.vec, dv[d][i], dv[d][i + 1], dv[d][i + 2], dv[d][i + 3]);
+    }
+}
+
+// ---------------------------------------------------------------- launchers
+
+inline unsigned grid_of(int64_t n) { return (unsigned)n; }
+constexpr int64_t kMaxGrid = (1 << 23);
+
+template <class Tag, int DP, int WK>
+hipError_t launch_fwd_rows(const AttnArgs &a, hipStream_t stream) {
+  using F = FwdShape<Tag, DP, WK>;
+  const int64_t n = (int64_t)((a.R + F::BM - 1) / F::BM) * a.splits * a.B * a.Hk;
+  if (n > kMaxGrid) return hipErrorInvalidConfiguration;
+  attn_fwd_kernel<Tag, DP, WK><<<grid_of(n), 256, F::LDS, stream>>>(a);
+  return hipGetLastError();
+}
+
+template <class Tag, int DP>
+hipError_t launch_fwd(const AttnArgs &a, hipStream_t stream) {
+  hipError_t e;
+  if (a.R <= 32) {
+    constexpr int tiles = 4 * 32 * Tile<Tag, DP>::PITCH, joined = 4 * 32 * (DP + 4) * 4 + 1024;
+    constexpr int LDS = tiles > joined ? tiles : joined;
+    const int64_t n = (int64_t)a.splits * a.B * a.Hk;
+    if (n > kMaxGrid) return hipErrorInvalidConfiguration;
+    attn_token_kernel<Tag, DP><<<grid_of(n), 256, LDS, stream>>>(a);
+    e = hipGetLastError();
+  } else if (a.R <= 64) {
+    e = launch_fwd_rows<Tag, DP, 2>(a, stream);
+  } else {
+    e = launch_fwd_rows<Tag, DP, 1>(a, stream);
+  }
+  if (e != hipSuccess || a.splits == 1) return e;
+  const int64_t n = (a.B * a.Hk * (int64_t)a.R * a.D + 255) / 256;
+  if (n > kMaxGrid) return hipErrorInvalidConfiguration;
+  attn_join_kernel<Tag><<<grid_of(n), 256, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+template <class Tag, int DP>
+hipError_t launch_bwd(const AttnArgs &a, hipStream_t stream) {
+  const int64_t bh = a.B * a.Hk;
+  hipError_t e;
+  if (a.R > 0) {
+    const int64_t n = (bh * a.R + 15) / 16, m = bh * ((a.R + 127) / 128);
+    if (n > kMaxGrid || m > kMaxGrid) return hipErrorInvalidConfiguration;
+    attn_rowstat_kernel<Tag><<<grid_of(n), 256, 0, stream>>>(a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    attn_dq_kernel<Tag, DP><<<grid_of(m), 256, DqShape<Tag, DP>::LDS, stream>>>(a);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (a.Sk == 0) return hipSuccess;
+  const int64_t n = bh * ((a.Sk + 127) / 128) * a.row_parts;
+  if (n > kMaxGrid) return hipErrorInvalidConfiguration;
+  attn_dkv_kernel<Tag, DP><<<grid_of(n), 256, DkvShape<Tag, DP>::LDS, stream>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+template <class Tag>
+hipError_t AttnEntry<Tag>::forward(const AttnArgs &a, hipStream_t stream) {
+  if (a.D <= 32) return launch_fwd<Tag, 32>(a, stream);
+  if (a.D <= 64) return launch_fwd<Tag, 64>(a, stream);
+  if (a.D <= 96) return launch_fwd<Tag, 96>(a, stream);
+  return launch_fwd<Tag, 128>(a, stream);
+}
+
+template <class Tag>
+hipError_t AttnEntry<Tag>::backward(const AttnArgs &a, hipStream_t stream) {
+  if (a.D <= 32) return launch_bwd<Tag, 32>(a, stream);
+  if (a.D <= 64) return launch_bwd<Tag, 64>(a, stream);
+  if (a.D <= 96) return launch_bwd<Tag, 96>(a, stream);
+  return launch_bwd<Tag, 128>(a, stream);
+}
+
+}  // namespace wbmm

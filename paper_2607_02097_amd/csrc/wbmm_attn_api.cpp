@@ -1,0 +1,343 @@
+// C-ABI front end of the rotary positions and the cross attention: argument
+// validation, status codes and dispatch.  As in wbmm_api.cpp, every check runs
+// on the host before any GPU work is enqueued; nothing here allocates, prints
+// or aborts.
+#include <math.h>
+#include <stdint.h>
+
+#include "wbmm.h"
+#include "wbmm_attn_internal.h"
+
+namespace {
+
+using wbmm::AttnArgs;
+using wbmm::AttnEntry;
+using wbmm::Dt;
+using wbmm::RotaryArgs;
+using wbmm::Tokens;
+
+int64_t elem_size(int64_t dtype) { return dtype == WBMM_F32 ? 4 : dtype == WBMM_BF16 || dtype == WBMM_F16 ? 2 : 0; }
+
+bool aligned(const void *p, size_t a) { return ((uintptr_t)p % a) == 0; }
+
+wbmm_status from_hip(hipError_t e) {
+  // a grid past the launch limits is a shape without a kernel
+  return e == hipSuccess ? WBMM_OK : e == hipErrorInvalidConfiguration ? WBMM_ERR_UNSUPPORTED : WBMM_ERR_HIP;
+}
+
+// Addresses that a strided [B, S, H, D] tensor reaches, in bytes.
+struct Span {
+  uintptr_t at;
+  int64_t bytes;           // of the whole range
+  int64_t b, s, token;     // strides of entries and tokens, range of one token
+};
+
+constexpr int64_t kFar = (int64_t)1 << 46;  // bytes; keeps every offset far from overflow
+
+// Checks a tensor of n elements in each dimension and describes it.
+bool describe(const wbmm_tokens &t, int64_t B, int64_t S, int64_t H, int64_t D, int64_t es, Tokens *out, Span *sp) {
+  const int64_t st[3] = {t.stride_b, t.stride_s, t.stride_h}, n[3] = {B, S, H};
+  int64_t far = D;
+  for (int i = 0; i < 3; ++i) {
+    if (st[i] < 0) return false;
+    if (n[i] > 1) {
+      if (st[i] > kFar / (n[i] - 1)) return false;
+      far += st[i] * (n[i] - 1);
+    }
+    if (far > kFar) return false;
+  }
+  const bool empty = B == 0 || S == 0;
+  if (!empty && (!t.data || !aligned(t.data, (size_t)es))) return false;
+  // a stride over a single element is never taken
+  *out = {(char *)t.data, B > 1 ? st[0] * es : 0, S > 1 ? st[1] * es : 0, H > 1 ? st[2] * es : 0};
+  *sp = {(uintptr_t)t.data, empty ? 0 : far * es, out->b, out->s, ((H - 1) * (H > 1 ? st[2] : 0) + D) * es};
+  return true;
+}
+
+// An output's elements must not share an address.
+bool folds(const Tokens &t, int64_t B, int64_t S, int64_t H, int64_t D, int64_t es) {
+  if (B == 0 || S == 0) return false;
+  // dimensions in the order of their strides, each past the whole of the ones below
+  int64_t st[3] = {t.b, t.s, t.h}, n[3] = {B, S, H}, reach = D * es;
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 3; ++j)
+      if (st[j] < st[i]) {
+        const int64_t a = st[i], c = n[i];
+        st[i] = st[j], n[i] = n[j], st[j] = a, n[j] = c;
+      }
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] <= 1) continue;
+    if (st[i] < reach) return true;
+    reach += st[i] * (n[i] - 1);
+  }
+  return false;
+}
+
+bool clash(const Span &a, const Span &b) {
+  if (a.bytes == 0 || b.bytes == 0) return false;
+  if (a.at + (uintptr_t)a.bytes <= b.at || b.at + (uintptr_t)b.bytes <= a.at) return false;
+  // slices of one joint tensor: tokens at the same distances, separate parts
+  if (a.s == b.s && a.s > 0 && (a.b == 0 || a.b % a.s == 0) && (b.b == 0 || b.b % b.s == 0)) {
+    const int64_t d = (int64_t)((b.at - a.at) % (uintptr_t)a.s);
+    const int64_t shift = b.at >= a.at ? d : (int64_t)((a.s - (int64_t)((a.at - b.at) % (uintptr_t)a.s)) % a.s);
+    if (shift >= a.token && shift + b.token <= a.s) return false;
+  }
+  return true;
+}
+
+wbmm_status rotary(const wbmm_rotary_args *g, void *stream, int reverse) {
+  if (!g) return WBMM_ERR_INVALID_ARG;
+  const int64_t es = elem_size(g->dtype);
+  if (!es) return WBMM_ERR_UNSUPPORTED;
+  if (g->B < 0 || g->S < 0 || g->H <= 0 || g->D <= 0 || g->axes <= 0) return WBMM_ERR_INVALID_ARG;
+  if (g->axes > wbmm::kMaxAxes || g->D > wbmm::kMaxRotaryDim || g->H > INT32_MAX / g->D) return WBMM_ERR_UNSUPPORTED;
+  if (g->position_bytes != 4 && g->position_bytes != 8) return WBMM_ERR_INVALID_ARG;
+  RotaryArgs a = {};
+  int64_t pairs = 0;
+  for (int i = 0; i < g->axes; ++i) {
+    if (g->sections[i] < 0 || g->sections[i] > g->D) return WBMM_ERR_INVALID_ARG;
+    pairs += g->sections[i];
+    a.first[i] = (int)pairs;
+  }
+  if (pairs < 1 || 2 * pairs > g->D) return WBMM_ERR_INVALID_ARG;
+  if (pairs > wbmm::kMaxPairs) return WBMM_ERR_UNSUPPORTED;
+  if (g->pos_stride_a < 0 || g->pos_stride_b < 0 || g->pos_stride_s < 0) return WBMM_ERR_INVALID_ARG;
+  Span x, y;
+  if (!describe(g->x, g->B, g->S, g->H, g->D, es, &a.x, &x) || !describe(g->y, g->B, g->S, g->H, g->D, es, &a.y, &y))
+    return WBMM_ERR_INVALID_ARG;
+  if (folds(a.y, g->B, g->S, g->H, g->D, es)) return WBMM_ERR_INVALID_ARG;
+  if (g->B == 0 || g->S == 0) return WBMM_OK;
+  if (g->B > kFar / g->S) return WBMM_ERR_UNSUPPORTED;
+  if (!g->positions || !g->freqs || !aligned(g->positions, (size_t)g->position_bytes) || !aligned(g->freqs, 4))
+    return WBMM_ERR_INVALID_ARG;
+  const bool in_place = a.x.p == a.y.p && a.x.b == a.y.b && a.x.s == a.y.s && a.x.h == a.y.h;
+  if (!in_place && clash(x, y)) return WBMM_ERR_INVALID_ARG;
+  const int64_t n[3] = {g->axes, g->B, g->S}, st[3] = {g->pos_stride_a, g->pos_stride_b, g->pos_stride_s};
+  int64_t far = 1;
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] > 1 && st[i] > kFar / (n[i] - 1)) return WBMM_ERR_INVALID_ARG;
+    far += st[i] * (n[i] - 1);
+  }
+  const Span pos = {(uintptr_t)g->positions, far * g->position_bytes, 0, 0, 0};
+  const Span fr = {(uintptr_t)g->freqs, pairs * 4, 0, 0, 0};
+  if (clash(y, pos) || clash(y, fr)) return WBMM_ERR_INVALID_ARG;
+  a.pos = g->positions;
+  a.pos_a = g->pos_stride_a, a.pos_b = g->pos_stride_b, a.pos_s = g->pos_stride_s;
+  a.pos64 = g->position_bytes == 8;
+  a.freqs = g->freqs;
+  a.B = g->B, a.S = g->S;
+  a.H = (int)g->H, a.D = (int)g->D, a.P = (int)pairs, a.axes = (int)g->axes;
+  a.adjacent = g->adjacent != 0;
+  a.reverse = reverse;
+  return from_hip(wbmm::launch_rotary((Dt)g->dtype, a, (hipStream_t)stream));
+}
+
+// Sizes of an attention call; fills everything but the tensors.
+wbmm_status attn_sizes(const wbmm_cross_attention_args *g, AttnArgs *a) {
+  if (!g) return WBMM_ERR_INVALID_ARG;
+  if (!elem_size(g->dtype)) return WBMM_ERR_UNSUPPORTED;
+  if (g->B < 0 || g->Sq < 0 || g->Sk < 0 || g->Hq <= 0 || g->Hk <= 0 || g->D <= 0) return WBMM_ERR_INVALID_ARG;
+  if (g->Hq % g->Hk != 0) return WBMM_ERR_INVALID_ARG;
+  if (!(g->scale > 0) || !isfinite((float)g->scale) || (float)g->scale == 0.f) return WBMM_ERR_INVALID_ARG;
+  if (g->D > wbmm::kMaxHeadDim) return WBMM_ERR_UNSUPPORTED;
+  // rows of a key head and states are counted in 32 bits, with room to spare
+  const int64_t lim = (int64_t)1 << 30, G = g->Hq / g->Hk;
+  if (g->B > lim || g->Hq > lim || g->Sk > lim || (g->Sq > 0 && G > lim / g->Sq)) return WBMM_ERR_UNSUPPORTED;
+  if (g->B > 0 && g->Hq > lim / g->B) return WBMM_ERR_UNSUPPORTED;
+  if (g->mask_stride_b < 0 || g->mask_stride_s < 0) return WBMM_ERR_INVALID_ARG;
+  if (g->kv_lens && !aligned(g->kv_lens, 4)) return WBMM_ERR_INVALID_ARG;
+  *a = AttnArgs{};
+  a->B = g->B;
+  a->Sq = (int)g->Sq, a->Sk = (int)g->Sk, a->Hq = (int)g->Hq, a->Hk = (int)g->Hk, a->G = (int)G, a->D = (int)g->D;
+  a->R = (int)(g->Sq * G);
+  a->scale = (float)g->scale;
+  a->c = (float)(g->scale * 1.4426950408889634074);
+  if (!isfinite(a->c) || a->c == 0.f) return WBMM_ERR_INVALID_ARG;
+  a->lens = g->kv_lens;
+  a->mask = g->key_mask;
+  a->mask_b = g->mask_stride_b, a->mask_s = g->mask_stride_s;
+  a->splits = a->row_parts = 1;
+  return WBMM_OK;
+}
+
+int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
+
+struct FwdSpace {
+  int64_t part_o, part_l, total;
+};
+FwdSpace forward_space(const AttnArgs &a) {
+  FwdSpace w = {0, 0, 0};
+  if (a.splits > 1) {
+    const int64_t rows = (int64_t)a.splits * a.B * a.Hk * a.R;
+    w.part_l = up16(rows * a.D * 4);
+    w.total = w.part_l + up16(rows * 4);
+  }
+  return w;
+}
+struct BwdSpace {
+  int64_t part_dk, part_dv, total;
+};
+BwdSpace backward_space(const AttnArgs &a) {
+  BwdSpace w;
+  w.part_dk = up16(a.B * a.Hk * (int64_t)a.R * 8);
+  const int64_t part = a.row_parts > 1 ? up16((int64_t)a.row_parts * a.B * a.Hk * a.Sk * a.D * 4) : 0;
+  w.part_dv = w.part_dk + part;
+  w.total = w.part_dv + part;
+  return w;
+}
+
+bool rows16(const Tokens *const *t, int n, int64_t row) {
+  bool ok = row % 16 == 0;
+  for (int i = 0; i < n; ++i) ok = ok && ((uintptr_t)t[i]->p | t[i]->b | t[i]->s | t[i]->h) % 16 == 0;
+  return ok;
+}
+
+void plan_forward(Dt dt, AttnArgs *a) { a->splits = wbmm::attn_splits(dt, a->B, a->Sq, a->Sk, a->Hq, a->Hk); }
+void plan_backward(Dt dt, AttnArgs *a) { a->row_parts = wbmm::attn_row_parts(dt, a->B, a->Sq, a->Sk, a->Hq, a->Hk); }
+
+bool clash_any(const Span &o, const Span *in, int n) {
+  for (int i = 0; i < n; ++i)
+    if (clash(o, in[i])) return true;
+  return false;
+}
+
+Span flat(const void *p, int64_t bytes) { return {(uintptr_t)p, p ? bytes : 0, 0, 0, 0}; }
+
+// lens, mask and workspace as address ranges.
+void side_spans(const wbmm_cross_attention_args *g, Span *sp) {
+  sp[0] = flat(g->kv_lens, g->B * 4);
+  sp[1] = flat(g->key_mask, g->B && g->Sk ? (g->B - 1) * g->mask_stride_b + (g->Sk - 1) * g->mask_stride_s + 1 : 0);
+}
+
+bool mask_far(const wbmm_cross_attention_args *g) {
+  return (g->B > 1 && g->mask_stride_b > kFar / (g->B - 1)) || (g->Sk > 1 && g->mask_stride_s > kFar / (g->Sk - 1));
+}
+
+template <class F32, class BF16, class F16>
+hipError_t by_dtype(int64_t dtype, F32 f32, BF16 bf16, F16 f16) {
+  return dtype == WBMM_F32 ? f32() : dtype == WBMM_BF16 ? bf16() : f16();
+}
+
+}  // namespace
+
+extern "C" {
+
+wbmm_status wbmm_rotary_forward(const wbmm_rotary_args *args, void *stream) { return rotary(args, stream, 0); }
+
+wbmm_status wbmm_rotary_backward(const wbmm_rotary_args *args, void *stream) { return rotary(args, stream, 1); }
+
+size_t wbmm_cross_attention_forward_workspace_bytes(const wbmm_cross_attention_args *g) {
+  AttnArgs a;
+  if (attn_sizes(g, &a) != WBMM_OK) return 0;
+  plan_forward((Dt)g->dtype, &a);
+  return (size_t)forward_space(a).total;
+}
+
+wbmm_status wbmm_cross_attention_forward(const wbmm_cross_attention_args *g, void *stream) {
+  AttnArgs a;
+  wbmm_status s = attn_sizes(g, &a);
+  if (s != WBMM_OK) return s;
+  const int64_t es = elem_size(g->dtype);
+  Span in[5], out;
+  if (!describe(g->q, g->B, g->Sq, g->Hq, g->D, es, &a.q, &in[0]) ||
+      !describe(g->k, g->B, g->Sk, g->Hk, g->D, es, &a.k, &in[1]) ||
+      !describe(g->v, g->B, g->Sk, g->Hk, g->D, es, &a.v, &in[2]) ||
+      !describe(g->out, g->B, g->Sq, g->Hq, g->D, es, &a.o, &out) || mask_far(g))
+    return WBMM_ERR_INVALID_ARG;
+  side_spans(g, in + 3);
+  const Span lse = flat(g->lse, g->B * g->Hq * g->Sq * 4);
+  if (g->lse && !aligned(g->lse, 4)) return WBMM_ERR_INVALID_ARG;
+  if (folds(a.o, g->B, g->Sq, g->Hq, g->D, es) || clash_any(out, in, 5) || clash_any(lse, in, 5) || clash(out, lse))
+    return WBMM_ERR_INVALID_ARG;
+  if (g->B == 0 || g->Sq == 0) return WBMM_OK;
+  plan_forward((Dt)g->dtype, &a);
+  const FwdSpace w = forward_space(a);
+  if (w.total > 0) {
+    const Span ws = flat(g->workspace, w.total);
+    if (!g->workspace || g->workspace_bytes < w.total || !aligned(g->workspace, 16) || clash_any(ws, in, 5) ||
+        clash(ws, out) || clash(ws, lse))
+      return WBMM_ERR_INVALID_ARG;
+    a.part_o = (float *)((char *)g->workspace + w.part_o);
+    a.part_l = (float *)((char *)g->workspace + w.part_l);
+  }
+  a.lse = g->lse;
+  const Tokens *t[] = {&a.q, &a.k, &a.v, &a.o};
+  a.vec = rows16(t, 4, g->D * es);
+  const hipStream_t st = (hipStream_t)stream;
+  return from_hip(by_dtype(
+      g->dtype, [&] { return AttnEntry<wbmm::TagF32>::forward(a, st); },
+      [&] { return AttnEntry<wbmm::TagBF16>::forward(a, st); }, [&] { return AttnEntry<wbmm::TagF16>::forward(a, st); }));
+}
+
+size_t wbmm_cross_attention_backward_workspace_bytes(const wbmm_cross_attention_args *g) {
+  AttnArgs a;
+  if (attn_sizes(g, &a) != WBMM_OK) return 0;
+  plan_backward((Dt)g->dtype, &a);
+  return (size_t)backward_space(a).total;
+}
+
+wbmm_status wbmm_cross_attention_backward(const wbmm_cross_attention_args *g, void *stream) {
+  AttnArgs a;
+  wbmm_status s = attn_sizes(g, &a);
+  if (s != WBMM_OK) return s;
+  const int64_t es = elem_size(g->dtype);
+  Span in[8], out[3];
+  if (!describe(g->q, g->B, g->Sq, g->Hq, g->D, es, &a.q, &in[0]) ||
+      !describe(g->k, g->B, g->Sk, g->Hk, g->D, es, &a.k, &in[1]) ||
+      !describe(g->v, g->B, g->Sk, g->Hk, g->D, es, &a.v, &in[2]) ||
+      !describe(g->out, g->B, g->Sq, g->Hq, g->D, es, &a.o, &in[3]) ||
+      !describe(g->dout, g->B, g->Sq, g->Hq, g->D, es, &a.dout, &in[4]) ||
+      !describe(g->dq, g->B, g->Sq, g->Hq, g->D, es, &a.dq, &out[0]) ||
+      !describe(g->dk, g->B, g->Sk, g->Hk, g->D, es, &a.dk, &out[1]) ||
+      !describe(g->dv, g->B, g->Sk, g->Hk, g->D, es, &a.dv, &out[2]) || mask_far(g))
+    return WBMM_ERR_INVALID_ARG;
+  side_spans(g, in + 5);
+  in[7] = flat(g->lse, g->B * g->Hq * g->Sq * 4);
+  if (g->B > 0 && g->Sq > 0 && (!g->lse || !aligned(g->lse, 4))) return WBMM_ERR_INVALID_ARG;
+  if (folds(a.dq, g->B, g->Sq, g->Hq, g->D, es) || folds(a.dk, g->B, g->Sk, g->Hk, g->D, es) ||
+      folds(a.dv, g->B, g->Sk, g->Hk, g->D, es))
+    return WBMM_ERR_INVALID_ARG;
+  for (const Span &o : out)
+    if (clash_any(o, in, 8)) return WBMM_ERR_INVALID_ARG;
+  if (clash(out[0], out[1]) || clash(out[0], out[2]) || clash(out[1], out[2])) return WBMM_ERR_INVALID_ARG;
+  if (g->B == 0 || (g->Sq == 0 && g->Sk == 0)) return WBMM_OK;
+  plan_backward((Dt)g->dtype, &a);
+  const BwdSpace w = backward_space(a);
+  if (w.total > 0) {
+    const Span ws = flat(g->workspace, w.total);
+    if (!g->workspace || g->workspace_bytes < w.total || !aligned(g->workspace, 16) || clash_any(ws, in, 8) ||
+        clash_any(ws, out, 3))
+      return WBMM_ERR_INVALID_ARG;
+    a.rowstat = (float2 *)g->workspace;
+    a.part_dk = (float *)((char *)g->workspace + w.part_dk);
+    a.part_dv = (float *)((char *)g->workspace + w.part_dv);
+  }
+  a.lse = g->lse;
+  const Tokens *t[] = {&a.q, &a.k, &a.v, &a.o, &a.dout, &a.dq, &a.dk, &a.dv};
+  a.vec = rows16(t, 8, g->D * es);
+  const hipStream_t st = (hipStream_t)stream;
+  return from_hip(by_dtype(
+      g->dtype, [&] { return AttnEntry<wbmm::TagF32>::backward(a, st); },
+      [&] { return AttnEntry<wbmm::TagBF16>::backward(a, st); },
+      [&] { return AttnEntry<wbmm::TagF16>::backward(a, st); }));
+}
+
+}  // extern "C"
+
+namespace wbmm {
+
+// A token's kernel reads the states once and has nothing to share, so its
+// parts are as many as fill the chip's 256 compute units twice, of 256 states
+// (two blocks a wave) at least; a part more costs a partial result and the
+// joining launch.
+int attn_splits(Dt, int64_t B, int Sq, int Sk, int Hq, int Hk) {
+  const int64_t rows = (int64_t)Sq * (Hq / Hk), units = B * Hk;
+  if (rows > 32 || units <= 0) return 1;
+  const int64_t want = 512 / units, most = Sk / 256;
+  const int64_t n = want < most ? want : most;
+  return n < 1 ? 1 : (int)n;
+}
+
+int attn_row_parts(Dt, int64_t, int, int, int, int) { return 1; }
+
+}  // namespace wbmm
