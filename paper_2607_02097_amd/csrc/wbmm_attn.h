@@ -242,23 +242,31 @@ struct Mover {
 };
 
 // Rows first .. first + ROWS - 1 of the states of one head: those from `end`
-// on, and masked ones, as zeros (what lies there may be anything).
+// on, and masked ones, as zeros (what lies there may be anything).  The mask's
+// bytes travel with the rows and are looked at when the rows are written to
+// LDS, so that nothing waits for them earlier.
 template <class Tag, int DP, int ROWS, int THREADS>
 struct StateMover : Mover<Tag, DP, ROWS, THREADS> {
   using M = Mover<Tag, DP, ROWS, THREADS>;
+  uint8_t seen[M::NP];
   __device__ void load(const char *base, int64_t stride, int first, int end, const uint8_t *mask, int64_t mask_s, int D,
                        int vec, int tid) {
     const int d0 = M::chunk(tid) * M::T::CE;
 #pragma unroll
     for (int p = 0; p < M::NP; ++p) {
       const int j = first + M::row(tid, p);
-      u32x4 v = {0, 0, 0, 0};
-      if (j < end && (ROWS % M::RPP == 0 || M::row(tid, p) < ROWS)) {
-        v = load_chunk<Tag>(base + j * stride, d0, D, vec);
-        if (mask && !mask[j * mask_s]) v = (u32x4){0, 0, 0, 0};
-      }
-      this->r[p] = v;
+      const bool in = j < end && (ROWS % M::RPP == 0 || M::row(tid, p) < ROWS);
+      this->r[p] = in ? load_chunk<Tag>(base + j * stride, d0, D, vec) : (u32x4){0, 0, 0, 0};
+      if (mask) seen[p] = in ? mask[j * mask_s] : 0;
     }
+  }
+  __device__ void store_seen(char *tile, int tid, bool masked) {
+    if (masked) {
+#pragma unroll
+      for (int p = 0; p < M::NP; ++p)
+        if (!seen[p]) this->r[p] = (u32x4){0, 0, 0, 0};
+    }
+    this->store(tile, tid);
   }
 };
 
@@ -393,8 +401,8 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   }
   for (int t = t0; t < t1; ++t) {
     char *kt = smem + (t & 1) * 2 * F::TILE, *vt = kt + F::TILE;
-    mk.store(kt, tid);
-    mv.store(vt, tid);
+    mk.store_seen(kt, tid, mask != nullptr);
+    mv.store_seen(vt, tid, mask != nullptr);
     __syncthreads();
     if (t + 1 < t1) {
       mk.load(kb, a.k.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, a.vec, tid);
@@ -547,7 +555,7 @@ __global__ __launch_bounds__(256, 2) void attn_token_kernel(AttnArgs a) {
 #pragma unroll
     for (int u = 0; u < T::NU; ++u) s = mma_chunk<Tag>(kf[u], qf[u], s);
     if (t + 4 < t1) load_k(t + 4);
-    mv.store(vt, lane);
+    mv.store_seen(vt, lane, mask != nullptr);
     if (t + 4 < t1) mv.load(vb, a.v.s, (t + 4) * 32, len, mask, a.mask_s, a.D, a.vec, lane);
     if (a.mask || (t + 1) * 32 > len) {
       const uint32_t bits = (uint32_t)visible(a, b, t * 32, 32, len, lane) >> (4 * h);
@@ -740,8 +748,8 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs
   }
   for (int t = 0; t < t1; ++t) {
     char *kt = smem + (t & 1) * 2 * F::TILE, *vt = kt + F::TILE;
-    mk.store(kt, tid);
-    mv.store(vt, tid);
+    mk.store_seen(kt, tid, mask != nullptr);
+    mv.store_seen(vt, tid, mask != nullptr);
     __syncthreads();
     if (t + 1 < t1) {
       mk.load(kb, a.k.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, a.vec, tid);
@@ -787,7 +795,11 @@ template <class Tag, int DP>
 struct DkvShape {
   static constexpr int BR = 32;
   static constexpr int TILE = BR * Tile<Tag, DP>::PITCH;
-  static constexpr int STAT = 4 * TILE;  // two row statistics tiles behind the tiles
+  // 16-bit heads of more than 64 components: the values' fragments are read
+  // from LDS each time, so that two waves fit a SIMD.
+  static constexpr bool VLDS = Tag::W16 && DP > 64;
+  static constexpr int VAL = 4 * TILE;
+  static constexpr int STAT = VAL + (VLDS ? 128 * Tile<Tag, DP>::PITCH : 0);  // two tiles of row statistics
   static constexpr int LDS = STAT + 2 * 2 * BR * 4;
 };
 
@@ -810,7 +822,7 @@ struct RowMover : Mover<Tag, DP, ROWS, 256> {
 };
 
 template <class Tag, int DP>
-__global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArgs a) {
   using T = Tile<Tag, DP>;
   using F = DkvShape<Tag, DP>;
   constexpr int DT = T::DT;
@@ -834,14 +846,20 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnArgs a) {
 
   bool see = j < len;
   if (a.mask && see) see = a.mask[b * a.mask_b + j * a.mask_s] != 0;
-  u32x4 kf[T::NU], vf[T::NU];
+  u32x4 kf[T::NU], vf[F::VLDS ? 1 : T::NU];
+  const int rowlane = T::rowlane(lane), collane = T::collane(lane);
+  char *const val = smem + F::VAL + wave * 32 * T::PITCH;  // this wave's values
   {
     const char *kr = a.k.p + b * a.k.b + hk * a.k.h + j * a.k.s, *vr = a.v.p + b * a.v.b + hk * a.v.h + j * a.v.s;
 #pragma unroll
     for (int u = 0; u < T::NU; ++u) {
       const int d0 = (2 * u + h) * T::CE;
       kf[u] = see ? load_chunk<Tag>(kr, d0, a.D, a.vec) : (u32x4){0, 0, 0, 0};
-      vf[u] = see ? load_chunk<Tag>(vr, d0, a.D, a.vec) : (u32x4){0, 0, 0, 0};
+      const u32x4 v = see ? load_chunk<Tag>(vr, d0, a.D, a.vec) : (u32x4){0, 0, 0, 0};
+      if constexpr (F::VLDS)
+        *(u32x4 *)(val + (rowlane ^ (u << 5))) = v;
+      else
+        vf[u] = v;
     }
   }
   RowMover<Tag, DP, F::BR> mq, mg;
@@ -851,7 +869,6 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnArgs a) {
     mg.load(a, a.dout, b, hk, t * F::BR, a.R, tid);
     if (tid < F::BR) st = t * F::BR + tid < a.R ? a.rowstat[bh * a.R + t * F::BR + tid] : make_float2(INFINITY, 0.f);
   };
-  const int rowlane = T::rowlane(lane), collane = T::collane(lane);
   f32x16 dk[DT] = {}, dv[DT] = {};
   if (t0 < t1) load(t0);
   for (int t = t0; t < t1; ++t) {
@@ -866,7 +883,14 @@ __global__ __launch_bounds__(256, 1) void attn_dkv_kernel(AttnArgs a) {
     __syncthreads();
     if (t + 1 < t1) load(t + 1);
     f32x16 s = rows_product<Tag, DP>(qt, rowlane, 0, kf);
-    f32x16 dp = rows_product<Tag, DP>(gt, rowlane, 0, vf);
+    f32x16 dp = {};
+    if constexpr (F::VLDS) {
+#pragma unroll
+      for (int u = 0; u < T::NU; ++u)
+        dp = mma_chunk<Tag>(*(const u32x4 *)(gt + (rowlane ^ (u << 5))), *(const u32x4 *)(val + (rowlane ^ (u << 5))), dp);
+    } else {
+      dp = rows_product<Tag, DP>(gt, rowlane, 0, vf);
+    }
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
       const f32x4 l4 = *(const f32x4 *)(stat + 2 * i + 4 * h);
