@@ -37,7 +37,8 @@ HIP_FLAGS = ["--offload-arch=" + ARCH, "-O3", "-std=c++20", "-fPIC",
 # parallel; the largest windows (slowest units) first.
 UNITS = [("wbmm_inst.hip", ["-DWBMM_INST_TAG=%s" % tag, "-DWBMM_INST_LO=%d" % lo])
          for lo in (13, 9, 5, 1) for tag in ("TagBF16", "TagF16", "TagF32")]
-UNITS += [("wbmm_attn.hip", ["-DWBMM_INST_TAG=%s" % tag]) for tag in ("TagF32", "TagBF16", "TagF16")]
+UNITS += [("wbmm_attn.hip", ["-DWBMM_INST_TAG=%s" % tag, "-DWBMM_INST_VEC=%d" % vec])
+          for tag in ("TagF32", "TagBF16", "TagF16") for vec in (1, 0)]
 UNITS += [("wbmm_gen.hip", ["-DWBMM_INST_TAG=%s" % tag]) for tag in ("TagF32", "TagBF16", "TagF16")]
 UNITS += [("wbmm_dense.hip", []), ("wbmm_reduce.hip", []), ("wbmm_noalloc.hip", []), ("wbmm_rotary.hip", []),
           ("wbmm_dispatch.cpp", []), ("wbmm_api.cpp", []), ("wbmm_attn_api.cpp", [])]

@@ -178,12 +178,14 @@ __device__ inline void cols_product(const char *tile, int collane, int base, con
 // ------------------------------------------------------------------- memory
 
 // Chunk (16 bytes from component d0 on) of a row of D components; what lies
-// past D is zero.  VEC: rows are whole 16-byte pieces.
-template <class Tag>
-__device__ inline u32x4 load_chunk(const char *row, int d0, int D, int vec) {
+// past D is zero.  VEC: rows are whole 16-byte pieces.  (A template parameter
+// of the kernels: with both forms in one kernel, short calls spent more time
+// on fetching code than on their work.)
+template <class Tag, bool VEC>
+__device__ inline u32x4 load_chunk(const char *row, int d0, int D) {
   u32x4 v = {0, 0, 0, 0};
   if (d0 >= D) return v;
-  if (vec) return *(const u32x4 *)(row + d0 * Tag::ES);
+  if constexpr (VEC) return *(const u32x4 *)(row + d0 * Tag::ES);
   if constexpr (Tag::W16) {
     const u16 *p = (const u16 *)row + d0;
 #pragma unroll
@@ -198,28 +200,67 @@ __device__ inline u32x4 load_chunk(const char *row, int d0, int D, int vec) {
   return v;
 }
 
-// Four consecutive components of a row, rounded once, stored from d0 on.
-template <class Tag>
-__device__ inline void store4(char *row, int d0, int D, int vec, float a, float b, float c, float d) {
+template <class Tag, bool VEC>
+__device__ inline void store_chunk(char *row, int d0, int D, u32x4 v) {
   if (d0 >= D) return;
-  const float f[4] = {a, b, c, d};
-  if constexpr (Tag::W16) {
-    const uint32_t lo = pack2<Tag>(a, b), hi = pack2<Tag>(c, d);
-    if (vec) {
-      *(u32x2 *)(row + d0 * 2) = (u32x2){lo, hi};
-    } else {
-      const u16 e[4] = {(u16)lo, (u16)(lo >> 16), (u16)hi, (u16)(hi >> 16)};
+  if constexpr (VEC) {
+    *(u32x4 *)(row + d0 * Tag::ES) = v;
+  } else if constexpr (Tag::W16) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (d0 + j < D) ((u16 *)row)[d0 + j] = e[j];
-    }
-  } else if (vec) {
-    *(f32x4 *)(row + d0 * 4) = (f32x4){a, b, c, d};
+    for (int j = 0; j < 8; ++j)
+      if (d0 + j < D) ((u16 *)row)[d0 + j] = (u16)(v[j / 2] >> (16 * (j & 1)));
   } else {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-      if (d0 + j < D) ((float *)row)[d0 + j] = f[j];
+      if (d0 + j < D) ((uint32_t *)row)[d0 + j] = v[j];
   }
+}
+
+template <class Tag> __device__ inline void store1(char *row, int d, float v) {
+  if constexpr (Tag::W16)
+    ((u16 *)row)[d] = (u16)pack2<Tag>(v, 0.f);
+  else
+    ((float *)row)[d] = v;
+}
+
+// Order between a wave's own writes and reads of LDS that no other wave uses.
+__device__ inline void wave_lds_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Results of 32 rows (lane: row l % 32, components 32 dt + 8 (i / 4) + 4 h +
+// i % 4), multiplied by f, rounded once and stored through this wave's piece of
+// LDS (32 rows), so that each row leaves in whole 16-byte pieces of
+// neighbouring lanes.  row_at(n): address of row n, or null.
+template <class Tag, int DP, bool VEC, class RowAt>
+__device__ inline void store_rows(char *piece, const f32x16 *acc, float f, int D, int lane, RowAt row_at) {
+  using T = Tile<Tag, DP>;
+  const int h = lane >> 5, l31 = lane & 31;
+#pragma unroll
+  for (int dt = 0; dt < T::DT; ++dt)
+#pragma unroll
+    for (int i = 0; i < 16; i += 4) {
+      const float a = acc[dt][i] * f, b = acc[dt][i + 1] * f, c = acc[dt][i + 2] * f, d = acc[dt][i + 3] * f;
+      const int byte = (32 * dt + 2 * i + 4 * h) * Tag::ES;  // a half chunk (16-bit) or a chunk
+      char *at = piece + l31 * T::PITCH + ((((byte >> 4) ^ T::swz(l31)) << 4) | (byte & 15));
+      if constexpr (Tag::W16)
+        *(u32x2 *)at = (u32x2){pack2<Tag>(a, b), pack2<Tag>(c, d)};
+      else
+        *(f32x4 *)at = (f32x4){a, b, c, d};
+    }
+  wave_lds_fence();
+  constexpr int RPP = 64 / T::LPC;
+  const int c = lane % T::LPC;
+#pragma unroll
+  for (int p = 0; p < 32 / RPP; ++p) {
+    const int rw = p * RPP + lane / T::LPC;
+    char *row = row_at(rw);
+    if (row)
+      store_chunk<Tag, VEC>(row, c * T::CE, D, *(const u32x4 *)(piece + rw * T::PITCH + ((c ^ T::swz(rw)) << 4)));
+  }
+  wave_lds_fence();
 }
 
 // A tile of ROWS rows on its way from memory to LDS through registers.
@@ -245,18 +286,18 @@ struct Mover {
 // on, and masked ones, as zeros (what lies there may be anything).  The mask's
 // bytes travel with the rows and are looked at when the rows are written to
 // LDS, so that nothing waits for them earlier.
-template <class Tag, int DP, int ROWS, int THREADS>
+template <class Tag, int DP, bool VEC, int ROWS, int THREADS>
 struct StateMover : Mover<Tag, DP, ROWS, THREADS> {
   using M = Mover<Tag, DP, ROWS, THREADS>;
   uint8_t seen[M::NP];
   __device__ void load(const char *base, int64_t stride, int first, int end, const uint8_t *mask, int64_t mask_s, int D,
-                       int vec, int tid) {
+                       int tid) {
     const int d0 = M::chunk(tid) * M::T::CE;
 #pragma unroll
     for (int p = 0; p < M::NP; ++p) {
       const int j = first + M::row(tid, p);
       const bool in = j < end && (ROWS % M::RPP == 0 || M::row(tid, p) < ROWS);
-      this->r[p] = in ? load_chunk<Tag>(base + j * stride, d0, D, vec) : (u32x4){0, 0, 0, 0};
+      this->r[p] = in ? load_chunk<Tag, VEC>(base + j * stride, d0, D) : (u32x4){0, 0, 0, 0};
       if (mask) seen[p] = in ? mask[j * mask_s] : 0;
     }
   }
@@ -309,7 +350,7 @@ __device__ inline int length_of(const AttnArgs &a, int64_t b) {
 
 // Row fragments of 32 rows of a group (second operand): lane l has chunks
 // 2 u + h of row r (nothing for r >= R).
-template <class Tag, int DP>
+template <class Tag, int DP, bool VEC>
 __device__ inline void load_rows(const AttnArgs &a, const Tokens &t, int64_t b, int hk, int r, int lane, u32x4 *f) {
   using T = Tile<Tag, DP>;
   const int h = lane >> 5;
@@ -317,11 +358,18 @@ __device__ inline void load_rows(const AttnArgs &a, const Tokens &t, int64_t b, 
     const int s = r / a.G, g = r - s * a.G;
     const char *row = t.p + b * t.b + s * t.s + (int64_t)(hk * a.G + g) * t.h;
 #pragma unroll
-    for (int u = 0; u < T::NU; ++u) f[u] = load_chunk<Tag>(row, (2 * u + h) * T::CE, a.D, a.vec);
+    for (int u = 0; u < T::NU; ++u) f[u] = load_chunk<Tag, VEC>(row, (2 * u + h) * T::CE, a.D);
   } else {
 #pragma unroll
     for (int u = 0; u < T::NU; ++u) f[u] = (u32x4){0, 0, 0, 0};
   }
+}
+
+// Address of row r of a group in an output, or null past the last.
+__device__ inline char *group_row(const AttnArgs &a, const Tokens &t, int64_t b, int hk, int r) {
+  if (r >= a.R) return nullptr;
+  const int s = r / a.G, g = r - s * a.G;
+  return t.p + b * t.b + s * t.s + (int64_t)(hk * a.G + g) * t.h;
 }
 
 // Scores of 32 states (one lane: 16 of one query) to weights: running maximum
@@ -364,7 +412,7 @@ struct FwdShape {
   static constexpr int LDS = 4 * TILE;
 };
 
-template <class Tag, int DP, int WK>
+template <class Tag, int DP, int WK, bool VEC>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   using T = Tile<Tag, DP>;
   using F = FwdShape<Tag, DP, WK>;
@@ -374,39 +422,35 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wr = wave % F::WR, wk = wave / F::WR, h = lane >> 5;
   const int tiles = (a.R + F::BM - 1) / F::BM;
-  int64_t unit = unit_of(blockIdx.x, gridDim.x);
-  const int rt = (int)(unit % tiles);
-  unit /= tiles;
-  const int split = (int)(unit % a.splits);
-  const int64_t bh = unit / a.splits;
+  const int64_t unit = unit_of(blockIdx.x, gridDim.x), bh = unit / tiles;
+  const int rt = (int)(unit - bh * tiles);
   const int64_t b = bh / a.Hk;
   const int hk = (int)(bh - b * a.Hk);
   const int len = length_of(a, b);
-  const int all = (len + F::BN - 1) / F::BN;
-  const int t0 = (int)((int64_t)all * split / a.splits), t1 = (int)((int64_t)all * (split + 1) / a.splits);
+  const int t1 = (len + F::BN - 1) / F::BN;
   const int r = rt * F::BM + wr * 32 + (lane & 31);
 
   u32x4 qf[T::NU];
-  load_rows<Tag, DP>(a, a.q, b, hk, r, lane, qf);
+  load_rows<Tag, DP, VEC>(a, a.q, b, hk, r, lane, qf);
   const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
   const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
-  StateMover<Tag, DP, F::BN, 256> mk, mv;
+  StateMover<Tag, DP, VEC, F::BN, 256> mk, mv;
   const int rowlane = T::rowlane(lane), collane = T::collane(lane);
 
   f32x16 acc[DT] = {};
   float top = -INFINITY, sum = 0.f;
-  if (t0 < t1) {
-    mk.load(kb, a.k.s, t0 * F::BN, len, mask, a.mask_s, a.D, a.vec, tid);
-    mv.load(vb, a.v.s, t0 * F::BN, len, mask, a.mask_s, a.D, a.vec, tid);
+  if (t1 > 0) {
+    mk.load(kb, a.k.s, 0, len, mask, a.mask_s, a.D, tid);
+    mv.load(vb, a.v.s, 0, len, mask, a.mask_s, a.D, tid);
   }
-  for (int t = t0; t < t1; ++t) {
+  for (int t = 0; t < t1; ++t) {
     char *kt = smem + (t & 1) * 2 * F::TILE, *vt = kt + F::TILE;
     mk.store_seen(kt, tid, mask != nullptr);
     mv.store_seen(vt, tid, mask != nullptr);
     __syncthreads();
     if (t + 1 < t1) {
-      mk.load(kb, a.k.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, a.vec, tid);
-      mv.load(vb, a.v.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, a.vec, tid);
+      mk.load(kb, a.k.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, tid);
+      mv.load(vb, a.v.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, tid);
     }
     f32x16 s[NB];
 #pragma unroll
@@ -464,8 +508,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
       o[(16 * DT + 1) * 64] = sum;
     }
     __syncthreads();
-    if (wk > 0) return;
-    for (int w = 1; w < WK; ++w) {
+    for (int w = 1; w < (wk > 0 ? 0 : WK); ++w) {
       const float *o = xo + (wave + (w - 1) * F::WR) * PER + lane;
       const float top2 = o[16 * DT * 64], sum2 = o[(16 * DT + 1) * 64];
       const float t = fmaxf(top, top2);
@@ -478,48 +521,67 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
         for (int i = 0; i < 16; ++i) acc[d][i] = acc[d][i] * f1 + o[(d * 16 + i) * 64] * f2;
     }
   }
-  if (r >= a.R) return;
   // a row that sees nothing: zeros, and minus infinity
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  const float lse2 = sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum);
-  if (a.splits > 1) {
-    const int64_t at = (split * a.B * a.Hk + bh) * a.R + r;
-    if (h == 0) a.part_l[at] = lse2;
-    float *o = a.part_o + at * a.D;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; i += 4)
-        store4<TagF32>((char *)o, 32 * d + 8 * (i / 4) + 4 * h, a.D, a.D % 4 == 0, acc[d][i] * inv, acc[d][i + 1] * inv,
-                       acc[d][i + 2] * inv, acc[d][i + 3] * inv);
-    return;
+  if (a.lse && h == 0 && wk == 0 && r < a.R) {
+    const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
+    a.lse[(b * a.Hq + hq) * a.Sq + sq] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
   }
-  const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
-  if (a.lse && h == 0) a.lse[(b * a.Hq + hq) * a.Sq + sq] = lse2 * kLn2;
-  char *o = a.o.p + b * a.o.b + sq * a.o.s + hq * a.o.h;
-#pragma unroll
-  for (int d = 0; d < DT; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; i += 4)
-      store4<Tag>(o, 32 * d + 8 * (i / 4) + 4 * h, a.D, a.vec, acc[d][i] * inv, acc[d][i + 1] * inv, acc[d][i + 2] * inv,
-                  acc[d][i + 3] * inv);
+  __syncthreads();
+  if (wk > 0) return;
+  store_rows<Tag, DP, VEC>(smem + wave * 32 * T::PITCH, acc, inv, a.D, lane,
+                           [&](int n) { return group_row(a, a.o, b, hk, rt * F::BM + wr * 32 + n); });
 }
 
-// ------------------------------------------------- forward, a handful of rows
+// ------------------------------------------------------- forward, few rows
 
-// At most 32 rows a key head (single tokens, drafts): the states are read
-// once and bound the kernel.  Each wave runs over blocks of 32 states of its
-// own; keys go from memory straight into the product's first operand, values
-// through a piece of LDS that only this wave uses, so no barrier is needed.
+// Where the tiles of 128 rows would leave much of the chip idle (single
+// tokens above all, whose time is the reading of the states): a workgroup
+// takes 32 rows and a part of the states, in blocks of 32, and each of its
+// waves every fourth block.  Keys go from memory straight into the product's
+// first operand, values through a piece of LDS that only this wave uses, so
+// the loop has no barrier.  The waves' results are joined through LDS, the
+// parts' by attn_join_kernel.
 template <class Tag, int DP>
-__global__ __launch_bounds__(256, 2) void attn_token_kernel(AttnArgs a) {
+struct FewShape {
+  static constexpr int TILE = 32 * Tile<Tag, DP>::PITCH;
+  static constexpr int OP = DP + 4;  // floats of a row when joining
+  static int lds(int R) {
+    const int tiles = 4 * TILE, rows = R < 32 ? R : 32, join = (4 * rows * OP + 256) * 4;
+    return tiles > join ? tiles : join;
+  }
+};
+
+// Row fragments (first operand) of the 32 states from `first` on, zeros where
+// they are not visible.
+template <class Tag, int DP, bool VEC>
+__device__ inline void load_states(const AttnArgs &a, const char *base, int64_t stride, const uint8_t *mask, int first,
+                                   int len, int lane, u32x4 *f) {
   using T = Tile<Tag, DP>;
-  constexpr int DT = T::DT, TILE = 32 * T::PITCH;
+  const int h = lane >> 5, j = first + (lane & 31);
+  const bool in = j < len;
+#pragma unroll
+  for (int u = 0; u < T::NU; ++u)
+    f[u] = in ? load_chunk<Tag, VEC>(base + j * stride, (2 * u + h) * T::CE, a.D) : (u32x4){0, 0, 0, 0};
+  if (mask && in && !mask[j * a.mask_s]) {
+#pragma unroll
+    for (int u = 0; u < T::NU; ++u) f[u] = (u32x4){0, 0, 0, 0};
+  }
+}
+
+template <class Tag, int DP, bool VEC>
+__global__ __launch_bounds__(256, Tag::W16 || DP <= 64 ? 2 : 1) void attn_few_kernel(AttnArgs a) {
+  using T = Tile<Tag, DP>;
+  using F = FewShape<Tag, DP>;
+  constexpr int DT = T::DT;
   extern __shared__ __align__(512) char attn_smem[];
   char *const smem = attn_smem;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5, l31 = lane & 31;
+  const int tiles = (a.R + 31) / 32;
   int64_t unit = unit_of(blockIdx.x, gridDim.x);
+  const int rt = (int)(unit % tiles);
+  unit /= tiles;
   const int split = (int)(unit % a.splits);
   const int64_t bh = unit / a.splits;
   const int64_t b = bh / a.Hk;
@@ -527,36 +589,29 @@ __global__ __launch_bounds__(256, 2) void attn_token_kernel(AttnArgs a) {
   const int len = length_of(a, b);
   const int all = (len + 31) / 32;
   const int t0 = (int)((int64_t)all * split / a.splits), t1 = (int)((int64_t)all * (split + 1) / a.splits);
+  const int rows = a.R - rt * 32 < 32 ? a.R - rt * 32 : 32;
 
   u32x4 qf[T::NU], kf[T::NU];
-  load_rows<Tag, DP>(a, a.q, b, hk, l31, lane, qf);
   const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
   const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
-  StateMover<Tag, DP, 32, 64> mv;
-  char *vt = smem + wave * TILE;
+  StateMover<Tag, DP, VEC, 32, 64> mv;
+  char *vt = smem + wave * F::TILE;
   const int collane = T::collane(lane);
   f32x16 acc[DT] = {};
   float top = -INFINITY, sum = 0.f;
   int t = t0 + wave;
-  auto load_k = [&](int blk) {
-    const int j = blk * 32 + l31;
-    bool see = j < len;
-    if (mask && see) see = mask[j * a.mask_s] != 0;
-#pragma unroll
-    for (int u = 0; u < T::NU; ++u)
-      kf[u] = see ? load_chunk<Tag>(kb + j * a.k.s, (2 * u + h) * T::CE, a.D, a.vec) : (u32x4){0, 0, 0, 0};
-  };
   if (t < t1) {
-    load_k(t);
-    mv.load(vb, a.v.s, t * 32, len, mask, a.mask_s, a.D, a.vec, lane);
+    load_states<Tag, DP, VEC>(a, kb, a.k.s, mask, t * 32, len, lane, kf);
+    mv.load(vb, a.v.s, t * 32, len, mask, a.mask_s, a.D, lane);
   }
+  load_rows<Tag, DP, VEC>(a, a.q, b, hk, rt * 32 + l31, lane, qf);
   for (; t < t1; t += 4) {
     f32x16 s = {};
 #pragma unroll
     for (int u = 0; u < T::NU; ++u) s = mma_chunk<Tag>(kf[u], qf[u], s);
-    if (t + 4 < t1) load_k(t + 4);
+    if (t + 4 < t1) load_states<Tag, DP, VEC>(a, kb, a.k.s, mask, (t + 4) * 32, len, lane, kf);
     mv.store_seen(vt, lane, mask != nullptr);
-    if (t + 4 < t1) mv.load(vb, a.v.s, (t + 4) * 32, len, mask, a.mask_s, a.D, a.vec, lane);
+    if (t + 4 < t1) mv.load(vb, a.v.s, (t + 4) * 32, len, mask, a.mask_s, a.D, lane);
     if (a.mask || (t + 1) * 32 > len) {
       const uint32_t bits = (uint32_t)visible(a, b, t * 32, 32, len, lane) >> (4 * h);
 #pragma unroll
@@ -575,25 +630,18 @@ __global__ __launch_bounds__(256, 2) void attn_token_kernel(AttnArgs a) {
       s[i] = exp2_(__builtin_fmaf(s[i], a.c, -sub));
       sum += s[i];
     }
-    // this wave's writes to LDS come before its own reads
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    wave_lds_fence();
     const Weights<Tag> w = to_weights<Tag>(s);
     cols_product<Tag, DP>(vt, collane, 0, w, acc);
-    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+    wave_lds_fence();
   }
   sum = other_half_sum(sum);
 
-  // join the four waves: [wave][row][DP + 4] results, then each wave's top
-  // and sum per row
-  constexpr int OP = DP + 4;
-  float *xo = (float *)smem, *xt = xo + 4 * 32 * OP, *xs = xt + 128;
+  // join the four waves: [wave][row][OP] results, then tops and sums
+  float *xo = (float *)smem, *xt = xo + 4 * rows * F::OP, *xs = xt + 128;
   __syncthreads();
-  if (l31 < a.R) {
-    float *o = xo + (wave * 32 + l31) * OP;
+  if (l31 < rows) {
+    float *o = xo + (wave * rows + l31) * F::OP;
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -605,32 +653,30 @@ __global__ __launch_bounds__(256, 2) void attn_token_kernel(AttnArgs a) {
     }
   }
   __syncthreads();
-  for (int e = tid; e < a.R * DP; e += 256) {
-    const int r = e / DP, d = e % DP;
+  for (int e = tid; e < rows * DP; e += 256) {
+    const int n = e / DP, d = e % DP;
+    if (d >= a.D) continue;
     float t4 = -INFINITY, s4 = 0.f, o4 = 0.f;
 #pragma unroll
-    for (int w = 0; w < 4; ++w) t4 = fmaxf(t4, xt[w * 32 + r]);
+    for (int w = 0; w < 4; ++w) t4 = fmaxf(t4, xt[w * 32 + n]);
 #pragma unroll
     for (int w = 0; w < 4; ++w) {
-      const float tw = xt[w * 32 + r];
+      const float tw = xt[w * 32 + n];
       const float f = tw == t4 ? 1.f : exp2_(tw - t4);
-      s4 += xs[w * 32 + r] * f;
-      o4 += xo[(w * 32 + r) * OP + d] * f;
+      s4 += xs[w * 32 + n] * f;
+      o4 += xo[(w * rows + n) * F::OP + d] * f;
     }
-    if (d >= a.D) continue;
+    // a row that sees nothing: zeros, and minus infinity
     const float inv = s4 == 0.f ? 0.f : 1.f / s4;
     const float lse2 = s4 == 0.f ? -INFINITY : t4 + __builtin_amdgcn_logf(s4);
+    const int r = rt * 32 + n;
     if (a.splits > 1) {
       const int64_t at = (split * a.B * a.Hk + bh) * a.R + r;
       a.part_o[at * a.D + d] = o4 * inv;
       if (d == 0) a.part_l[at] = lse2;
     } else {
+      store1<Tag>(group_row(a, a.o, b, hk, r), d, o4 * inv);
       const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
-      char *o = a.o.p + b * a.o.b + sq * a.o.s + hq * a.o.h;
-      if constexpr (Tag::W16)
-        ((u16 *)o)[d] = (u16)pack2<Tag>(o4 * inv, 0.f);
-      else
-        ((float *)o)[d] = o4 * inv;
       if (a.lse && d == 0) a.lse[(b * a.Hq + hq) * a.Sq + sq] = lse2 * kLn2;
     }
   }
@@ -657,12 +703,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   o = sum == 0.f ? 0.f : o / sum;
   const int64_t bh = row / a.R, b = bh / a.Hk;
   const int r = (int)(row - bh * a.R), hk = (int)(bh - b * a.Hk);
+  store1<Tag>(group_row(a, a.o, b, hk, r), d, o);
   const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
-  char *p = a.o.p + b * a.o.b + sq * a.o.s + hq * a.o.h;
-  if constexpr (Tag::W16)
-    ((u16 *)p)[d] = (u16)pack2<Tag>(o, 0.f);
-  else
-    ((float *)p)[d] = o;
   if (a.lse && d == 0)
     a.lse[(b * a.Hq + hq) * a.Sq + sq] = (sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
@@ -675,76 +717,78 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 // dq, states for dk and dv), so every sum has one owner and a fixed order: no
 // atomics, and the same bits every time.
 
-// Per row {lse in log2 units, delta}; rows that see nothing get +infinity, so
-// that every weight comes out as zero.  Sixteen lanes a row.
-template <class Tag>
-__global__ __launch_bounds__(256) void attn_rowstat_kernel(AttnArgs a) {
-  constexpr int CE = 16 / Tag::ES;
-  const int64_t n = a.B * a.Hk * (int64_t)a.R;
-  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-  const int l = threadIdx.x & 15;
+// Statistics of the lane's row: {lse in log2 units, delta}; a row that sees
+// nothing gets +infinity, so that its weights come out as zero.  Kept for the
+// kernel of dk and dv by one lane a row (`keep`).
+template <class Tag, int DP, bool VEC>
+__device__ inline float2 row_stat(const AttnArgs &a, int64_t b, int hk, int r, int lane, const u32x4 *gf, bool keep) {
+  using T = Tile<Tag, DP>;
+  u32x4 of[T::NU];
+  load_rows<Tag, DP, VEC>(a, a.o, b, hk, r, lane, of);
   float d = 0.f;
-  const int64_t at = row < n ? row : n - 1;
-  const int64_t bh = at / a.R, b = bh / a.Hk;
-  const int r = (int)(at - bh * a.R), hk = (int)(bh - b * a.Hk);
-  const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
-  const char *o = a.o.p + b * a.o.b + sq * a.o.s + hq * a.o.h;
-  const char *g = a.dout.p + b * a.dout.b + sq * a.dout.s + hq * a.dout.h;
-  for (int c = l * CE; c < a.D; c += 16 * CE) {
-    const u32x4 x = load_chunk<Tag>(o, c, a.D, a.vec), y = load_chunk<Tag>(g, c, a.D, a.vec);
+#pragma unroll
+  for (int u = 0; u < T::NU; ++u)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-      if constexpr (Tag::W16) {
-        d += to_f32<Tag>((u16)(x[j] & 0xffff)) * to_f32<Tag>((u16)(y[j] & 0xffff));
-        d += to_f32<Tag>((u16)(x[j] >> 16)) * to_f32<Tag>((u16)(y[j] >> 16));
-      } else {
-        d += __uint_as_float(x[j]) * __uint_as_float(y[j]);
-      }
+      const uint32_t x = of[u][j], y = gf[u][j];
+      if constexpr (Tag::W16)
+        d += to_f32<Tag>((u16)(x & 0xffff)) * to_f32<Tag>((u16)(y & 0xffff)) +
+             to_f32<Tag>((u16)(x >> 16)) * to_f32<Tag>((u16)(y >> 16));
+      else
+        d += __uint_as_float(x) * __uint_as_float(y);
     }
-  }
-#pragma unroll
-  for (int m = 8; m; m >>= 1) d += __shfl_xor(d, m, 16);
-  if (l == 0 && row < n) {
+  d = other_half_sum(d);
+  float2 st = make_float2(INFINITY, 0.f);
+  if (r < a.R) {
+    const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
     const float lse = a.lse[(b * a.Hq + hq) * a.Sq + sq];
-    a.rowstat[row] = lse == -INFINITY ? make_float2(INFINITY, 0.f) : make_float2(lse * kLog2e, d);
+    if (lse != -INFINITY) st = make_float2(lse * kLog2e, d);
+    if (keep && lane < 32) a.rowstat[(b * a.Hk + hk) * a.R + r] = st;
+  }
+  return st;
+}
+
+// Scores to ds (one lane: 16 states of one row), zero where not visible.
+__device__ inline void to_ds(f32x16 *s, const f32x16 &dp, float c, float2 st, uint32_t seen, int h) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) (*s)[i] = exp2_(__builtin_fmaf((*s)[i], c, -st.x)) * (dp[i] - st.y);
+  if (seen != 0xffffffffu) {
+    const uint32_t bits = seen >> (4 * h);
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (!((bits >> (8 * (i / 4) + i % 4)) & 1)) (*s)[i] = 0.f;
   }
 }
 
-// dq: as the forward, a workgroup takes 128 rows and runs over all states.
-template <class Tag, int DP>
-struct DqShape {
-  static constexpr int BN = Tag::W16 ? 64 : 32;
-  static constexpr int TILE = BN * Tile<Tag, DP>::PITCH;
-  static constexpr int LDS = 4 * TILE;
-};
-
-template <class Tag, int DP>
+// dq: as the forward, a workgroup takes 32 (4 / WK) rows and runs over all
+// states, WK waves sharing rows and splitting each tile.
+template <class Tag, int DP, int WK, bool VEC>
 __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs a) {
   using T = Tile<Tag, DP>;
-  using F = DqShape<Tag, DP>;
-  constexpr int DT = T::DT, NB = F::BN / 32;
+  using F = FwdShape<Tag, DP, WK>;
+  constexpr int DT = T::DT, NB = F::NB;
   extern __shared__ __align__(512) char attn_smem[];
   char *const smem = attn_smem;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
-  const int tiles = (a.R + 127) / 128;
+  const int wr = wave % F::WR, wk = wave / F::WR;
+  const int tiles = (a.R + F::BM - 1) / F::BM;
   const int64_t unit = unit_of(blockIdx.x, gridDim.x), bh = unit / tiles, b = bh / a.Hk;
   const int rt = (int)(unit - bh * tiles), hk = (int)(bh - b * a.Hk);
   const int len = length_of(a, b);
   const int t1 = (len + F::BN - 1) / F::BN;
-  const int r = rt * 128 + wave * 32 + (lane & 31);
+  const int r = rt * F::BM + wr * 32 + (lane & 31);
   u32x4 qf[T::NU], gf[T::NU];
-  load_rows<Tag, DP>(a, a.q, b, hk, r, lane, qf);
-  load_rows<Tag, DP>(a, a.dout, b, hk, r, lane, gf);
-  float2 st = make_float2(INFINITY, 0.f);
-  if (r < a.R) st = a.rowstat[bh * a.R + r];
+  load_rows<Tag, DP, VEC>(a, a.q, b, hk, r, lane, qf);
+  load_rows<Tag, DP, VEC>(a, a.dout, b, hk, r, lane, gf);
+  const float2 st = row_stat<Tag, DP, VEC>(a, b, hk, r, lane, gf, wk == 0);
   const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
   const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
-  StateMover<Tag, DP, F::BN, 256> mk, mv;
+  StateMover<Tag, DP, VEC, F::BN, 256> mk, mv;
   const int rowlane = T::rowlane(lane), collane = T::collane(lane);
   f32x16 acc[DT] = {};
   if (t1 > 0) {
-    mk.load(kb, a.k.s, 0, len, mask, a.mask_s, a.D, a.vec, tid);
-    mv.load(vb, a.v.s, 0, len, mask, a.mask_s, a.D, a.vec, tid);
+    mk.load(kb, a.k.s, 0, len, mask, a.mask_s, a.D, tid);
+    mv.load(vb, a.v.s, 0, len, mask, a.mask_s, a.D, tid);
   }
   for (int t = 0; t < t1; ++t) {
     char *kt = smem + (t & 1) * 2 * F::TILE, *vt = kt + F::TILE;
@@ -752,39 +796,130 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs
     mv.store_seen(vt, tid, mask != nullptr);
     __syncthreads();
     if (t + 1 < t1) {
-      mk.load(kb, a.k.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, a.vec, tid);
-      mv.load(vb, a.v.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, a.vec, tid);
+      mk.load(kb, a.k.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, tid);
+      mv.load(vb, a.v.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, tid);
     }
     uint64_t see = ~(uint64_t)0;
-    if (a.mask || (t + 1) * F::BN > len) see = visible(a, b, t * F::BN, F::BN, len, lane);
+    if (a.mask || (t + 1) * F::BN > len) see = visible(a, b, t * F::BN, F::BN, len, lane) >> (wk * F::KW);
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
-      f32x16 s = rows_product<Tag, DP>(kt, rowlane, 32 * k, qf);
-      const f32x16 dp = rows_product<Tag, DP>(vt, rowlane, 32 * k, gf);
-#pragma unroll
-      for (int i = 0; i < 16; ++i) s[i] = exp2_(__builtin_fmaf(s[i], a.c, -st.x)) * (dp[i] - st.y);
-      const uint32_t seen = (uint32_t)(see >> (32 * k));
-      if (seen != 0xffffffffu) {
-        const uint32_t bits = seen >> (4 * h);
-#pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (!((bits >> (8 * (i / 4) + i % 4)) & 1)) s[i] = 0.f;
-      }
+      const int base = wk * F::KW + 32 * k;
+      f32x16 s = rows_product<Tag, DP>(kt, rowlane, base, qf);
+      const f32x16 dp = rows_product<Tag, DP>(vt, rowlane, base, gf);
+      to_ds(&s, dp, a.c, st, (uint32_t)(see >> (32 * k)), h);
       // ds is rounded to the inputs' type for its product
       const Weights<Tag> w = to_weights<Tag>(s);
-      cols_product<Tag, DP>(kt, collane, 32 * k, w, acc);
+      cols_product<Tag, DP>(kt, collane, base, w, acc);
     }
   }
-  if (r >= a.R) return;
-  const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
-  char *o = a.dq.p + b * a.dq.b + sq * a.dq.s + hq * a.dq.h;
-  const float f = a.scale;
+  __syncthreads();
+  if constexpr (WK > 1) {
+    float *xo = (float *)smem;  // [wave][16 DT][64]
+    constexpr int PER = 16 * DT * 64;
+    static_assert((4 - F::WR) * PER * 4 <= F::LDS, "the waves' results fit the tiles' space");
+    if (wk > 0) {
+      float *o = xo + (wave - F::WR) * PER + lane;
 #pragma unroll
-  for (int d = 0; d < DT; ++d)
+      for (int d = 0; d < DT; ++d)
 #pragma unroll
-    for (int i = 0; i < 16; i += 4)
-      store4<Tag>(o, 32 * d + 8 * (i / 4) + 4 * h, a.D, a.vec, acc[d][i] * f, acc[d][i + 1] * f, acc[d][i + 2] * f,
-                  acc[d][i + 3] * f);
+        for (int i = 0; i < 16; ++i) o[(d * 16 + i) * 64] = acc[d][i];
+    }
+    __syncthreads();
+    for (int w = 1; w < (wk > 0 ? 0 : WK); ++w) {
+      const float *o = xo + (wave + (w - 1) * F::WR) * PER + lane;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[d][i] += o[(d * 16 + i) * 64];
+    }
+    __syncthreads();
+    if (wk > 0) return;
+  }
+  store_rows<Tag, DP, VEC>(smem + wave * 32 * T::PITCH, acc, a.scale, a.D, lane,
+                           [&](int n) { return group_row(a, a.dq, b, hk, rt * F::BM + wr * 32 + n); });
+}
+
+// dq, few rows: as attn_few_kernel.  A block's keys are written to this wave's
+// piece of LDS from the fragments of the first product.
+template <class Tag, int DP, bool VEC>
+__global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_few_dq_kernel(AttnArgs a) {
+  using T = Tile<Tag, DP>;
+  using F = FewShape<Tag, DP>;
+  constexpr int DT = T::DT;
+  extern __shared__ __align__(512) char attn_smem[];
+  char *const smem = attn_smem;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h = lane >> 5, l31 = lane & 31;
+  const int tiles = (a.R + 31) / 32;
+  int64_t unit = unit_of(blockIdx.x, gridDim.x);
+  const int rt = (int)(unit % tiles);
+  unit /= tiles;
+  const int split = (int)(unit % a.splits);
+  const int64_t bh = unit / a.splits;
+  const int64_t b = bh / a.Hk;
+  const int hk = (int)(bh - b * a.Hk);
+  const int len = length_of(a, b);
+  const int all = (len + 31) / 32;
+  const int t0 = (int)((int64_t)all * split / a.splits), t1 = (int)((int64_t)all * (split + 1) / a.splits);
+  const int rows = a.R - rt * 32 < 32 ? a.R - rt * 32 : 32;
+
+  u32x4 qf[T::NU], gf[T::NU], kf[T::NU], vf[T::NU];
+  const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
+  const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
+  load_rows<Tag, DP, VEC>(a, a.q, b, hk, rt * 32 + l31, lane, qf);
+  load_rows<Tag, DP, VEC>(a, a.dout, b, hk, rt * 32 + l31, lane, gf);
+  const float2 st = row_stat<Tag, DP, VEC>(a, b, hk, rt * 32 + l31, lane, gf, split == 0 && wave == 0);
+  char *kt = smem + wave * F::TILE;
+  const int rowlane = T::rowlane(lane), collane = T::collane(lane);
+  f32x16 acc[DT] = {};
+  int t = t0 + wave;
+  if (t < t1) {
+    load_states<Tag, DP, VEC>(a, kb, a.k.s, mask, t * 32, len, lane, kf);
+    load_states<Tag, DP, VEC>(a, vb, a.v.s, mask, t * 32, len, lane, vf);
+  }
+  for (; t < t1; t += 4) {
+    f32x16 s = {}, dp = {};
+#pragma unroll
+    for (int u = 0; u < T::NU; ++u) {
+      s = mma_chunk<Tag>(kf[u], qf[u], s);
+      *(u32x4 *)(kt + (rowlane ^ (u << 5))) = kf[u];
+    }
+    if (t + 4 < t1) load_states<Tag, DP, VEC>(a, kb, a.k.s, mask, (t + 4) * 32, len, lane, kf);
+#pragma unroll
+    for (int u = 0; u < T::NU; ++u) dp = mma_chunk<Tag>(vf[u], gf[u], dp);
+    if (t + 4 < t1) load_states<Tag, DP, VEC>(a, vb, a.v.s, mask, (t + 4) * 32, len, lane, vf);
+    uint32_t seen = 0xffffffffu;
+    if (a.mask || (t + 1) * 32 > len) seen = (uint32_t)visible(a, b, t * 32, 32, len, lane);
+    to_ds(&s, dp, a.c, st, seen, h);
+    wave_lds_fence();
+    const Weights<Tag> w = to_weights<Tag>(s);
+    cols_product<Tag, DP>(kt, collane, 0, w, acc);
+    wave_lds_fence();
+  }
+  float *xo = (float *)smem;
+  __syncthreads();
+  if (l31 < rows) {
+    float *o = xo + (wave * rows + l31) * F::OP;
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; i += 4)
+        *(f32x4 *)(o + 32 * d + 8 * (i / 4) + 4 * h) = (f32x4){acc[d][i], acc[d][i + 1], acc[d][i + 2], acc[d][i + 3]};
+  }
+  __syncthreads();
+  for (int e = tid; e < rows * DP; e += 256) {
+    const int n = e / DP, d = e % DP;
+    if (d >= a.D) continue;
+    float o = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) o += xo[(w * rows + n) * F::OP + d];
+    o *= a.scale;
+    const int r = rt * 32 + n;
+    if (a.splits > 1)
+      a.part_o[((split * a.B * a.Hk + bh) * a.R + r) * a.D + d] = o;
+    else
+      store1<Tag>(group_row(a, a.dq, b, hk, r), d, o);
+  }
 }
 
 // dk, dv: a workgroup takes 128 states, 32 a wave, and runs over the rows of
@@ -800,11 +935,12 @@ struct DkvShape {
   static constexpr bool VLDS = Tag::W16 && DP > 64;
   static constexpr int VAL = 4 * TILE;
   static constexpr int STAT = VAL + (VLDS ? 128 * Tile<Tag, DP>::PITCH : 0);  // two tiles of row statistics
-  static constexpr int LDS = STAT + 2 * 2 * BR * 4;
+  static constexpr int OUT = 32 * Tile<TagF32, DP>::PITCH;                    // a wave's results, float32
+  static constexpr int LDS = STAT + 2 * 2 * BR * 4 > 4 * OUT ? STAT + 2 * 2 * BR * 4 : 4 * OUT;
 };
 
 // Rows first .. first + ROWS - 1 of a group.
-template <class Tag, int DP, int ROWS>
+template <class Tag, int DP, bool VEC, int ROWS>
 struct RowMover : Mover<Tag, DP, ROWS, 256> {
   using M = Mover<Tag, DP, ROWS, 256>;
   __device__ void load(const AttnArgs &a, const Tokens &t, int64_t b, int hk, int first, int end, int tid) {
@@ -815,13 +951,13 @@ struct RowMover : Mover<Tag, DP, ROWS, 256> {
       this->r[p] = (u32x4){0, 0, 0, 0};
       if (r < end && (ROWS % M::RPP == 0 || M::row(tid, p) < ROWS)) {
         const int s = r / a.G, g = r - s * a.G;
-        this->r[p] = load_chunk<Tag>(t.p + b * t.b + s * t.s + (int64_t)(hk * a.G + g) * t.h, d0, a.D, a.vec);
+        this->r[p] = load_chunk<Tag, VEC>(t.p + b * t.b + s * t.s + (int64_t)(hk * a.G + g) * t.h, d0, a.D);
       }
     }
   }
 };
 
-template <class Tag, int DP>
+template <class Tag, int DP, bool VEC>
 __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArgs a) {
   using T = Tile<Tag, DP>;
   using F = DkvShape<Tag, DP>;
@@ -838,7 +974,7 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
   const int64_t bh = unit / a.row_parts, b = bh / a.Hk;
   const int hk = (int)(bh - b * a.Hk);
   const int len = length_of(a, b);
-  const int j = kt0 * 128 + wave * 32 + l31;
+  const int j0 = kt0 * 128 + wave * 32, j = j0 + l31;
   const int all = (a.R + F::BR - 1) / F::BR;
   const int t0 = (int)((int64_t)all * part / a.row_parts);
   int t1 = (int)((int64_t)all * (part + 1) / a.row_parts);
@@ -854,15 +990,15 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
 #pragma unroll
     for (int u = 0; u < T::NU; ++u) {
       const int d0 = (2 * u + h) * T::CE;
-      kf[u] = see ? load_chunk<Tag>(kr, d0, a.D, a.vec) : (u32x4){0, 0, 0, 0};
-      const u32x4 v = see ? load_chunk<Tag>(vr, d0, a.D, a.vec) : (u32x4){0, 0, 0, 0};
+      kf[u] = see ? load_chunk<Tag, VEC>(kr, d0, a.D) : (u32x4){0, 0, 0, 0};
+      const u32x4 v = see ? load_chunk<Tag, VEC>(vr, d0, a.D) : (u32x4){0, 0, 0, 0};
       if constexpr (F::VLDS)
         *(u32x4 *)(val + (rowlane ^ (u << 5))) = v;
       else
         vf[u] = v;
     }
   }
-  RowMover<Tag, DP, F::BR> mq, mg;
+  RowMover<Tag, DP, VEC, F::BR> mq, mg;
   float2 st = make_float2(INFINITY, 0.f);
   auto load = [&](int t) {
     mq.load(a, a.q, b, hk, t * F::BR, a.R, tid);
@@ -907,111 +1043,126 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
     const Weights<Tag> wd = to_weights<Tag>(dp);
     cols_product<Tag, DP>(qt, collane, 0, wd, dk);
   }
-  if (j >= a.Sk) return;
-  // a state that is not visible has its column of results to itself: zeros
-  const float fk = a.scale;
+  if (!see) {
+    // a state that is not visible has its column of results to itself
+#pragma unroll
+    for (int d = 0; d < DT; ++d) dk[d] = dv[d] = (f32x16){};
+  }
+  __syncthreads();
   if (a.row_parts > 1) {
-    const int64_t at = ((part * a.B * a.Hk + bh) * a.Sk + j) * a.D;
-#pragma unroll
-    for (int d = 0; d < DT; ++d)
-#pragma unroll
-      for (int i = 0; i < 16; i += 4) {
-        const int d0 = 32 * d + 8 * (i / 4) + 4 * h, vec = a.D % 4 == 0;
-        store4<TagF32>((char *)(a.part_dk + at), d0, a.D, vec, dk[d][i] * fk, dk[d][i + 1] * fk, dk[d][i + 2] * fk,
-                       dk[d][i + 3] * fk);
-        store4<TagF32>((char *)(a.part_dv + at), d0, a.D, vec, dv[d][i], dv[d][i + 1], dv[d][i + 2], dv[d][i + 3]);
-      }
+    float *pk = a.part_dk + (part * a.B * a.Hk + bh) * a.Sk * a.D, *pv = a.part_dv + (pk - a.part_dk);
+    auto row = [&](float *p, int n) { return j0 + n < a.Sk ? (char *)(p + (int64_t)(j0 + n) * a.D) : nullptr; };
+    store_rows<TagF32, DP, VEC>(smem + wave * F::OUT, dk, a.scale, a.D, lane, [&](int n) { return row(pk, n); });
+    store_rows<TagF32, DP, VEC>(smem + wave * F::OUT, dv, 1.f, a.D, lane, [&](int n) { return row(pv, n); });
     return;
   }
-  char *ok = a.dk.p + b * a.dk.b + j * a.dk.s + hk * a.dk.h, *ov = a.dv.p + b * a.dv.b + j * a.dv.s + hk * a.dv.h;
-#pragma unroll
-  for (int d = 0; d < DT; ++d)
-#pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const int d0 = 32 * d + 8 * (i / 4) + 4 * h;
-      if (!see) {
-        store4<Tag>(ok, d0, a.D, a.vec, 0.f, 0.f, 0.f, 0.f);
-        store4<Tag>(ov, d0, a.D, a.vec, 0.f, 0.f, 0.f, 0.f);
-        continue;
-      }
-      store4<Tag>(ok, d0, a.D, a.vec, dk[d][i] * fk, dk[d][i + 1] * fk, dk[d][i + 2] * fk, dk[d][i + 3] * fk);
-      store4<Tag>(ov, d0, a.D, a.vec, dv[d][i], dv[d][i + 1], dv[d][i + 2], dv[d][i + 3]);
-    }
+  auto row = [&](const Tokens &t, int n) {
+    return j0 + n < a.Sk ? t.p + b * t.b + (j0 + n) * t.s + hk * t.h : nullptr;
+  };
+  store_rows<Tag, DP, VEC>(smem + wave * F::OUT, dk, a.scale, a.D, lane, [&](int n) { return row(a.dk, n); });
+  store_rows<Tag, DP, VEC>(smem + wave * F::OUT, dv, 1.f, a.D, lane, [&](int n) { return row(a.dv, n); });
+}
+
+// Sums of partial gradients, in the order of the parts: rows [B Hk, N] of D
+// components, row n of key head hk being token n / G of head hk G + n % G.
+// Blocks of y = 1 take the second tensor.
+struct SumArgs {
+  const float *part[2];
+  Tokens out[2];
+  int64_t rows;  // B Hk N
+  int parts, N, G, Hk, D;
+};
+
+template <class Tag>
+__global__ __launch_bounds__(256) void attn_sum_kernel(SumArgs a) {
+  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, n = a.rows * a.D;
+  if (e >= n) return;
+  const float *part = a.part[blockIdx.y];
+  const Tokens &t = a.out[blockIdx.y];
+  float sum = 0.f;
+  for (int p = 0; p < a.parts; ++p) sum += part[p * n + e];
+  const int64_t row = e / a.D, bh = row / a.N, b = bh / a.Hk;
+  const int d = (int)(e - row * a.D), r = (int)(row - bh * a.N), hk = (int)(bh - b * a.Hk);
+  const int s = r / a.G, g = r - s * a.G;
+  store1<Tag>(t.p + b * t.b + s * t.s + (int64_t)(hk * a.G + g) * t.h, d, sum);
 }
 
 // ---------------------------------------------------------------- launchers
 
-inline unsigned grid_of(int64_t n) { return (unsigned)n; }
-constexpr int64_t kMaxGrid = (1 << 23);
+constexpr int64_t kMaxGrid = 1 << 23;  // workgroups of 256 threads in a launch
 
-template <class Tag, int DP, int WK>
-hipError_t launch_fwd_rows(const AttnArgs &a, hipStream_t stream) {
-  using F = FwdShape<Tag, DP, WK>;
-  const int64_t n = (int64_t)((a.R + F::BM - 1) / F::BM) * a.splits * a.B * a.Hk;
-  if (n > kMaxGrid) return hipErrorInvalidConfiguration;
-  attn_fwd_kernel<Tag, DP, WK><<<grid_of(n), 256, F::LDS, stream>>>(a);
-  return hipGetLastError();
-}
+#define WBMM_ATTN_LAUNCH(kernel, n, lds, args)                       \
+  do {                                                               \
+    const int64_t n_ = (n);                                          \
+    if (n_ > kMaxGrid) return hipErrorInvalidConfiguration;          \
+    kernel<<<dim3((unsigned)n_), dim3(256), (lds), stream>>>(args);  \
+    const hipError_t e_ = hipGetLastError();                         \
+    if (e_ != hipSuccess) return e_;                                 \
+  } while (0)
 
-template <class Tag, int DP>
+template <class Tag, int DP, bool VEC>
 hipError_t launch_fwd(const AttnArgs &a, hipStream_t stream) {
-  hipError_t e;
-  if (a.R <= 32) {
-    constexpr int tiles = 4 * 32 * Tile<Tag, DP>::PITCH, joined = 4 * 32 * (DP + 4) * 4 + 1024;
-    constexpr int LDS = tiles > joined ? tiles : joined;
-    const int64_t n = (int64_t)a.splits * a.B * a.Hk;
-    if (n > kMaxGrid) return hipErrorInvalidConfiguration;
-    attn_token_kernel<Tag, DP><<<grid_of(n), 256, LDS, stream>>>(a);
-    e = hipGetLastError();
-  } else if (a.R <= 64) {
-    e = launch_fwd_rows<Tag, DP, 2>(a, stream);
+  const int64_t bh = a.B * a.Hk;
+  if (a.tile_rows == 32) {
+    WBMM_ATTN_LAUNCH((attn_few_kernel<Tag, DP, VEC>), bh * ((a.R + 31) / 32) * a.splits, (FewShape<Tag, DP>::lds(a.R)), a);
+    if (a.splits > 1) WBMM_ATTN_LAUNCH((attn_join_kernel<Tag>), (bh * a.R * a.D + 255) / 256, 0, a);
+  } else if (a.tile_rows == 64) {
+    WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 2, VEC>), bh * ((a.R + 63) / 64), (FwdShape<Tag, DP, 2>::LDS), a);
   } else {
-    e = launch_fwd_rows<Tag, DP, 1>(a, stream);
+    WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 1, VEC>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
   }
-  if (e != hipSuccess || a.splits == 1) return e;
-  const int64_t n = (a.B * a.Hk * (int64_t)a.R * a.D + 255) / 256;
-  if (n > kMaxGrid) return hipErrorInvalidConfiguration;
-  attn_join_kernel<Tag><<<grid_of(n), 256, 0, stream>>>(a);
-  return hipGetLastError();
+  return hipSuccess;
 }
 
-template <class Tag, int DP>
+template <class Tag, int DP, bool VEC>
 hipError_t launch_bwd(const AttnArgs &a, hipStream_t stream) {
   const int64_t bh = a.B * a.Hk;
-  hipError_t e;
   if (a.R > 0) {
-    const int64_t n = (bh * a.R + 15) / 16, m = bh * ((a.R + 127) / 128);
-    if (n > kMaxGrid || m > kMaxGrid) return hipErrorInvalidConfiguration;
-    attn_rowstat_kernel<Tag><<<grid_of(n), 256, 0, stream>>>(a);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    attn_dq_kernel<Tag, DP><<<grid_of(m), 256, DqShape<Tag, DP>::LDS, stream>>>(a);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
+    if (a.tile_rows == 32) {
+      WBMM_ATTN_LAUNCH((attn_few_dq_kernel<Tag, DP, VEC>), bh * ((a.R + 31) / 32) * a.splits,
+                       (FewShape<Tag, DP>::lds(a.R)), a);
+      if (a.splits > 1) {
+        const SumArgs s = {{a.part_o}, {a.dq}, bh * a.R, a.splits, a.R, a.G, a.Hk, a.D};
+        WBMM_ATTN_LAUNCH((attn_sum_kernel<Tag>), (bh * a.R * a.D + 255) / 256, 0, s);
+      }
+    } else if (a.tile_rows == 64) {
+      WBMM_ATTN_LAUNCH((attn_dq_kernel<Tag, DP, 2, VEC>), bh * ((a.R + 63) / 64), (FwdShape<Tag, DP, 2>::LDS), a);
+    } else {
+      WBMM_ATTN_LAUNCH((attn_dq_kernel<Tag, DP, 1, VEC>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
+    }
   }
   if (a.Sk == 0) return hipSuccess;
-  const int64_t n = bh * ((a.Sk + 127) / 128) * a.row_parts;
-  if (n > kMaxGrid) return hipErrorInvalidConfiguration;
-  attn_dkv_kernel<Tag, DP><<<grid_of(n), 256, DkvShape<Tag, DP>::LDS, stream>>>(a);
-  return hipGetLastError();
+  WBMM_ATTN_LAUNCH((attn_dkv_kernel<Tag, DP, VEC>), bh * ((a.Sk + 127) / 128) * a.row_parts, (DkvShape<Tag, DP>::LDS), a);
+  if (a.row_parts > 1) {
+    const SumArgs s = {{a.part_dk, a.part_dv}, {a.dk, a.dv}, bh * a.Sk, a.row_parts, a.Sk, 1, a.Hk, a.D};
+    const int64_t n = (bh * a.Sk * a.D + 255) / 256;
+    if (n > kMaxGrid) return hipErrorInvalidConfiguration;
+    attn_sum_kernel<Tag><<<dim3((unsigned)n, 2), dim3(256), 0, stream>>>(s);
+    return hipGetLastError();
+  }
+  return hipSuccess;
 }
+
+#undef WBMM_ATTN_LAUNCH
 
 }  // namespace
 
 template <class Tag>
+template <bool VEC>
 hipError_t AttnEntry<Tag>::forward(const AttnArgs &a, hipStream_t stream) {
-  if (a.D <= 32) return launch_fwd<Tag, 32>(a, stream);
-  if (a.D <= 64) return launch_fwd<Tag, 64>(a, stream);
-  if (a.D <= 96) return launch_fwd<Tag, 96>(a, stream);
-  return launch_fwd<Tag, 128>(a, stream);
+  if (a.D <= 32) return launch_fwd<Tag, 32, VEC>(a, stream);
+  if (a.D <= 64) return launch_fwd<Tag, 64, VEC>(a, stream);
+  if (a.D <= 96) return launch_fwd<Tag, 96, VEC>(a, stream);
+  return launch_fwd<Tag, 128, VEC>(a, stream);
 }
 
 template <class Tag>
+template <bool VEC>
 hipError_t AttnEntry<Tag>::backward(const AttnArgs &a, hipStream_t stream) {
-  if (a.D <= 32) return launch_bwd<Tag, 32>(a, stream);
-  if (a.D <= 64) return launch_bwd<Tag, 64>(a, stream);
-  if (a.D <= 96) return launch_bwd<Tag, 96>(a, stream);
-  return launch_bwd<Tag, 128>(a, stream);
+  if (a.D <= 32) return launch_bwd<Tag, 32, VEC>(a, stream);
+  if (a.D <= 64) return launch_bwd<Tag, 64, VEC>(a, stream);
+  if (a.D <= 96) return launch_bwd<Tag, 96, VEC>(a, stream);
+  return launch_bwd<Tag, 128, VEC>(a, stream);
 }
 
 }  // namespace wbmm

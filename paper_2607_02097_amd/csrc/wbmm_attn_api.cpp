@@ -156,17 +156,17 @@ wbmm_status attn_sizes(const wbmm_cross_attention_args *g, AttnArgs *a) {
   a->lens = g->kv_lens;
   a->mask = g->key_mask;
   a->mask_b = g->mask_stride_b, a->mask_s = g->mask_stride_s;
-  a->splits = a->row_parts = 1;
   return WBMM_OK;
 }
 
 int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 
-struct FwdSpace {
-  int64_t part_o, part_l, total;
+// Space of a planned call.
+struct Space {
+  int64_t part_o, part_l, part_dk, part_dv, total;
 };
-FwdSpace forward_space(const AttnArgs &a) {
-  FwdSpace w = {0, 0, 0};
+Space forward_space(const AttnArgs &a) {
+  Space w = {};
   if (a.splits > 1) {
     const int64_t rows = (int64_t)a.splits * a.B * a.Hk * a.R;
     w.part_l = up16(rows * a.D * 4);
@@ -174,15 +174,14 @@ FwdSpace forward_space(const AttnArgs &a) {
   }
   return w;
 }
-struct BwdSpace {
-  int64_t part_dk, part_dv, total;
-};
-BwdSpace backward_space(const AttnArgs &a) {
-  BwdSpace w;
-  w.part_dk = up16(a.B * a.Hk * (int64_t)a.R * 8);
+Space backward_space(const AttnArgs &a) {
+  Space w = {};
+  // dq's partial sums are spent before those of dk and dv are written
+  w.part_o = w.part_dk = up16(a.B * a.Hk * (int64_t)a.R * 8);
+  const int64_t dq = a.splits > 1 ? up16((int64_t)a.splits * a.B * a.Hk * a.R * a.D * 4) : 0;
   const int64_t part = a.row_parts > 1 ? up16((int64_t)a.row_parts * a.B * a.Hk * a.Sk * a.D * 4) : 0;
   w.part_dv = w.part_dk + part;
-  w.total = w.part_dv + part;
+  w.total = w.part_o + (dq > 2 * part ? dq : 2 * part);
   return w;
 }
 
@@ -191,9 +190,6 @@ bool rows16(const Tokens *const *t, int n, int64_t row) {
   for (int i = 0; i < n; ++i) ok = ok && ((uintptr_t)t[i]->p | t[i]->b | t[i]->s | t[i]->h) % 16 == 0;
   return ok;
 }
-
-void plan_forward(Dt dt, AttnArgs *a) { a->splits = wbmm::attn_splits(dt, a->B, a->Sq, a->Sk, a->Hq, a->Hk); }
-void plan_backward(Dt dt, AttnArgs *a) { a->row_parts = wbmm::attn_row_parts(dt, a->B, a->Sq, a->Sk, a->Hq, a->Hk); }
 
 bool clash_any(const Span &o, const Span *in, int n) {
   for (int i = 0; i < n; ++i)
@@ -213,9 +209,16 @@ bool mask_far(const wbmm_cross_attention_args *g) {
   return (g->B > 1 && g->mask_stride_b > kFar / (g->B - 1)) || (g->Sk > 1 && g->mask_stride_s > kFar / (g->Sk - 1));
 }
 
-template <class F32, class BF16, class F16>
-hipError_t by_dtype(int64_t dtype, F32 f32, BF16 bf16, F16 f16) {
-  return dtype == WBMM_F32 ? f32() : dtype == WBMM_BF16 ? bf16() : f16();
+template <class Tag>
+hipError_t run(const AttnArgs &a, bool vec, bool back, hipStream_t st) {
+  if (back) return vec ? AttnEntry<Tag>::template backward<true>(a, st) : AttnEntry<Tag>::template backward<false>(a, st);
+  return vec ? AttnEntry<Tag>::template forward<true>(a, st) : AttnEntry<Tag>::template forward<false>(a, st);
+}
+
+hipError_t run(int64_t dtype, const AttnArgs &a, bool vec, bool back, hipStream_t st) {
+  return dtype == WBMM_F32    ? run<wbmm::TagF32>(a, vec, back, st)
+         : dtype == WBMM_BF16 ? run<wbmm::TagBF16>(a, vec, back, st)
+                              : run<wbmm::TagF16>(a, vec, back, st);
 }
 
 }  // namespace
@@ -229,7 +232,7 @@ wbmm_status wbmm_rotary_backward(const wbmm_rotary_args *args, void *stream) { r
 size_t wbmm_cross_attention_forward_workspace_bytes(const wbmm_cross_attention_args *g) {
   AttnArgs a;
   if (attn_sizes(g, &a) != WBMM_OK) return 0;
-  plan_forward((Dt)g->dtype, &a);
+  wbmm::attn_plan_forward((Dt)g->dtype, &a);
   return (size_t)forward_space(a).total;
 }
 
@@ -250,8 +253,8 @@ wbmm_status wbmm_cross_attention_forward(const wbmm_cross_attention_args *g, voi
   if (folds(a.o, g->B, g->Sq, g->Hq, g->D, es) || clash_any(out, in, 5) || clash_any(lse, in, 5) || clash(out, lse))
     return WBMM_ERR_INVALID_ARG;
   if (g->B == 0 || g->Sq == 0) return WBMM_OK;
-  plan_forward((Dt)g->dtype, &a);
-  const FwdSpace w = forward_space(a);
+  wbmm::attn_plan_forward((Dt)g->dtype, &a);
+  const Space w = forward_space(a);
   if (w.total > 0) {
     const Span ws = flat(g->workspace, w.total);
     if (!g->workspace || g->workspace_bytes < w.total || !aligned(g->workspace, 16) || clash_any(ws, in, 5) ||
@@ -262,17 +265,13 @@ wbmm_status wbmm_cross_attention_forward(const wbmm_cross_attention_args *g, voi
   }
   a.lse = g->lse;
   const Tokens *t[] = {&a.q, &a.k, &a.v, &a.o};
-  a.vec = rows16(t, 4, g->D * es);
-  const hipStream_t st = (hipStream_t)stream;
-  return from_hip(by_dtype(
-      g->dtype, [&] { return AttnEntry<wbmm::TagF32>::forward(a, st); },
-      [&] { return AttnEntry<wbmm::TagBF16>::forward(a, st); }, [&] { return AttnEntry<wbmm::TagF16>::forward(a, st); }));
+  return from_hip(run(g->dtype, a, rows16(t, 4, g->D * es), false, (hipStream_t)stream));
 }
 
 size_t wbmm_cross_attention_backward_workspace_bytes(const wbmm_cross_attention_args *g) {
   AttnArgs a;
   if (attn_sizes(g, &a) != WBMM_OK) return 0;
-  plan_backward((Dt)g->dtype, &a);
+  wbmm::attn_plan_backward((Dt)g->dtype, &a);
   return (size_t)backward_space(a).total;
 }
 
@@ -301,43 +300,66 @@ wbmm_status wbmm_cross_attention_backward(const wbmm_cross_attention_args *g, vo
     if (clash_any(o, in, 8)) return WBMM_ERR_INVALID_ARG;
   if (clash(out[0], out[1]) || clash(out[0], out[2]) || clash(out[1], out[2])) return WBMM_ERR_INVALID_ARG;
   if (g->B == 0 || (g->Sq == 0 && g->Sk == 0)) return WBMM_OK;
-  plan_backward((Dt)g->dtype, &a);
-  const BwdSpace w = backward_space(a);
+  wbmm::attn_plan_backward((Dt)g->dtype, &a);
+  const Space w = backward_space(a);
   if (w.total > 0) {
     const Span ws = flat(g->workspace, w.total);
     if (!g->workspace || g->workspace_bytes < w.total || !aligned(g->workspace, 16) || clash_any(ws, in, 8) ||
         clash_any(ws, out, 3))
       return WBMM_ERR_INVALID_ARG;
     a.rowstat = (float2 *)g->workspace;
+    a.part_o = (float *)((char *)g->workspace + w.part_o);
     a.part_dk = (float *)((char *)g->workspace + w.part_dk);
     a.part_dv = (float *)((char *)g->workspace + w.part_dv);
   }
   a.lse = g->lse;
   const Tokens *t[] = {&a.q, &a.k, &a.v, &a.o, &a.dout, &a.dq, &a.dk, &a.dv};
-  a.vec = rows16(t, 8, g->D * es);
-  const hipStream_t st = (hipStream_t)stream;
-  return from_hip(by_dtype(
-      g->dtype, [&] { return AttnEntry<wbmm::TagF32>::backward(a, st); },
-      [&] { return AttnEntry<wbmm::TagBF16>::backward(a, st); },
-      [&] { return AttnEntry<wbmm::TagF16>::backward(a, st); }));
+  return from_hip(run(g->dtype, a, rows16(t, 8, g->D * es), true, (hipStream_t)stream));
 }
 
 }  // extern "C"
 
 namespace wbmm {
 
-// A token's kernel reads the states once and has nothing to share, so its
-// parts are as many as fill the chip's 256 compute units twice, of 256 states
-// (two blocks a wave) at least; a part more costs a partial result and the
-// joining launch.
-int attn_splits(Dt, int64_t B, int Sq, int Sk, int Hq, int Hk) {
-  const int64_t rows = (int64_t)Sq * (Hq / Hk), units = B * Hk;
-  if (rows > 32 || units <= 0) return 1;
-  const int64_t want = 512 / units, most = Sk / 256;
-  const int64_t n = want < most ? want : most;
-  return n < 1 ? 1 : (int)n;
+namespace {
+
+constexpr int64_t kUnits = 256;  // compute units; two workgroups fit each
+
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+// Tiles of 128 rows run the matrix cores best, but want one for each compute
+// unit; below that, tiles of 32 rows whose states go in parts, as many as
+// give two workgroups a unit, of at least eight blocks (two a wave).
+void plan_rows(AttnArgs *a) {
+  const int64_t bh = a->B * a->Hk;
+  a->splits = 1;
+  if (a->R <= 64 && a->R > 32 && bh >= kUnits) {
+    a->tile_rows = 64;
+  } else if (a->R > 32 && bh * cdiv(a->R, 128) >= kUnits) {
+    a->tile_rows = 128;
+  } else {
+    a->tile_rows = 32;
+    const int64_t wgs = bh * cdiv(a->R, 32), most = a->Sk / 256;
+    int64_t n = wgs > 0 ? 2 * kUnits / wgs : 1;
+    n = n < most ? n : most;
+    a->splits = n < 1 ? 1 : (int)n;
+  }
 }
 
-int attn_row_parts(Dt, int64_t, int, int, int, int) { return 1; }
+}  // namespace
+
+void attn_plan_forward(Dt, AttnArgs *a) {
+  plan_rows(a);
+  a->row_parts = 1;
+}
+
+void attn_plan_backward(Dt, AttnArgs *a) {
+  plan_rows(a);
+  // dk, dv: parts of the rows until the chip is full, of at least four tiles
+  const int64_t wgs = a->B * a->Hk * cdiv(a->Sk, 128), most = a->R / 128;
+  int64_t n = wgs > 0 ? 2 * kUnits / wgs : 1;
+  n = n < most ? n : most;
+  a->row_parts = n < 1 ? 1 : (int)n;
+}
 
 }  // namespace wbmm

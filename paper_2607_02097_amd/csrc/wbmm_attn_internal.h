@@ -49,27 +49,28 @@ struct AttnArgs {
   int Sq, Sk, Hq, Hk, G, D;
   int R;  // rows of a key head: Sq * G, row r is query r / G of head r % G
   float scale, c;  // c = scale * log2(e)
-  // forward: the states of a sequence in `splits` parts with partial results
-  // part_o [splits, B Hk, R, D], part_l [splits, B Hk, R] (log2 units)
-  int splits;
+  // Rows of a workgroup's tile in the forward and for dq; with 32 of them the
+  // states go in `splits` parts with partial results part_o [splits, B Hk, R, D]
+  // and, forward, part_l [splits, B Hk, R] (lse in log2 units).
+  int tile_rows, splits;
   float *part_o, *part_l;
   // backward: per row {lse in log2 units, delta}, [B Hk, R]
   float2 *rowstat;
-  // backward: dk, dv in `row_parts` parts of the rows, partial sums float32
+  // backward: dk, dv in `row_parts` parts of the rows, with partial sums
   // part_dk, part_dv [row_parts, B Hk, Sk, D]
   int row_parts;
   float *part_dk, *part_dv;
-  int vec;  // 16-byte accesses to rows
 };
 
 template <class Tag>
 struct AttnEntry {
-  static hipError_t forward(const AttnArgs &a, hipStream_t stream);
-  static hipError_t backward(const AttnArgs &a, hipStream_t stream);
+  // VEC: rows of all tensors are whole 16-byte pieces
+  template <bool VEC> static hipError_t forward(const AttnArgs &a, hipStream_t stream);
+  template <bool VEC> static hipError_t backward(const AttnArgs &a, hipStream_t stream);
 };
 
-// Parts of the states in a forward call, of the rows in the dk / dv pass.
-int attn_splits(Dt dt, int64_t B, int Sq, int Sk, int Hq, int Hk);
-int attn_row_parts(Dt dt, int64_t B, int Sq, int Sk, int Hq, int Hk);
+// Tiles and parts of a call (functions of its sizes alone).
+void attn_plan_forward(Dt dt, AttnArgs *a);
+void attn_plan_backward(Dt dt, AttnArgs *a);
 
 }  // namespace wbmm
