@@ -116,14 +116,16 @@ template <class Tag> __device__ inline f32x16 mma_chunk(u32x4 a, u32x4 b, f32x16
 }
 
 // Result of a 32 x 32 product over the row fragments of an LDS tile (rows
-// base..base+31) with fragments in registers.
+// base..base+31) with fragments in registers; `at` is the tile's offset plus
+// rowlane().  (The tile is part of what the chunk's bits are xored into: the
+// address costs one instruction a read, and no registers between tiles.)
 template <class Tag, int DP>
-__device__ inline f32x16 rows_product(const char *tile, int rowlane, int base, const u32x4 *b) {
+__device__ inline f32x16 rows_product(const char *smem, int at, int base, const u32x4 *b) {
   using T = Tile<Tag, DP>;
   f32x16 acc = {};
 #pragma unroll
   for (int u = 0; u < T::NU; ++u) {
-    const u32x4 a = *(const u32x4 *)(tile + (rowlane ^ (u << 5)) + base * T::PITCH);
+    const u32x4 a = *(const u32x4 *)(smem + (at ^ (u << 5)) + base * T::PITCH);
     acc = mma_chunk<Tag>(a, b[u], acc);
   }
   return acc;
@@ -145,9 +147,10 @@ template <class Tag> __device__ inline Weights<Tag> to_weights(const f32x16 &p) 
   return r;
 }
 
-// acc[dt] += (columns of the LDS tile's rows base..base+31)^T weights.
+// acc[dt] += (columns of the LDS tile's rows base..base+31)^T weights; `at` is
+// the tile's offset plus collane().
 template <class Tag, int DP>
-__device__ inline void cols_product(const char *tile, int collane, int base, const Weights<Tag> &p, f32x16 *acc) {
+__device__ inline void cols_product(const char *smem, int at, int base, const Weights<Tag> &p, f32x16 *acc) {
   using T = Tile<Tag, DP>;
   if constexpr (Tag::W16) {
 #pragma unroll
@@ -158,7 +161,7 @@ __device__ inline void cols_product(const char *tile, int collane, int base, con
 #pragma unroll
         for (int g = 0; g < 2; ++g)
           v[g] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-              (lds_s16x4 *)(tile + (collane ^ (dt << 6) ^ (g << 5)) + (base + 16 * t + 8 * g) * T::PITCH));
+              (lds_s16x4 *)(smem + (at ^ (dt << 6) ^ (g << 5)) + (base + 16 * t + 8 * g) * T::PITCH));
         const u32x2 lo = __builtin_bit_cast(u32x2, v[0]), hi = __builtin_bit_cast(u32x2, v[1]);
         const u32x4 a = {lo[0], lo[1], hi[0], hi[1]};
         acc[dt] = mma_chunk<Tag>(a, p.w[t], acc[dt]);
@@ -169,7 +172,7 @@ __device__ inline void cols_product(const char *tile, int collane, int base, con
 #pragma unroll
       for (int dt = 0; dt < T::DT; ++dt) {
         const float a =
-            *(const float *)(tile + (collane ^ T::colxor32(dt, i)) + (base + 8 * (i / 4) + i % 4) * T::PITCH);
+            *(const float *)(smem + (at ^ T::colxor32(dt, i)) + (base + 8 * (i / 4) + i % 4) * T::PITCH);
         acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, p.w[i], acc[dt], 0, 0, 0);
       }
   }
@@ -272,6 +275,13 @@ struct Mover {
   u32x4 r[NP];
   __device__ static int chunk(int tid) { return tid % T::LPC; }
   __device__ static int row(int tid, int p) { return tid / T::LPC + p * RPP; }
+  // zeroes chunks past D
+  __device__ void cut(int D, int tid) {
+    if (D <= (T::LPC - 1) * T::CE && chunk(tid) * T::CE >= D) {
+#pragma unroll
+      for (int p = 0; p < NP; ++p) r[p] = (u32x4){0, 0, 0, 0};
+    }
+  }
   __device__ void store(char *tile, int tid) const {
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
@@ -282,32 +292,34 @@ struct Mover {
   }
 };
 
-// Rows first .. first + ROWS - 1 of the states of one head: those from `end`
-// on, and masked ones, as zeros (what lies there may be anything).  The mask's
-// bytes travel with the rows and are looked at when the rows are written to
-// LDS, so that nothing waits for them earlier.
+// Rows first .. first + ROWS - 1 of the states of one head.  Every lane loads:
+// rows from `end` on repeat the last one, chunks past D the row's first, so
+// the loads stand side by side without branches (rows in whole pieces; others
+// go element by element, under masks).  hide() zeroes what must not be seen on
+// the way to LDS: rows whose bit in `see` is not set, since a masked state may
+// hold anything, and chunks past D.
 template <class Tag, int DP, bool VEC, int ROWS, int THREADS>
 struct StateMover : Mover<Tag, DP, ROWS, THREADS> {
   using M = Mover<Tag, DP, ROWS, THREADS>;
-  uint8_t seen[M::NP];
-  __device__ void load(const char *base, int64_t stride, int first, int end, const uint8_t *mask, int64_t mask_s, int D,
-                       int tid) {
+  __device__ void load(const char *base, int64_t stride, int first, int end, int D, int tid) {
     const int d0 = M::chunk(tid) * M::T::CE;
+    if constexpr (VEC) base += (d0 < D ? d0 : 0) * Tag::ES;
 #pragma unroll
     for (int p = 0; p < M::NP; ++p) {
-      const int j = first + M::row(tid, p);
-      const bool in = j < end && (ROWS % M::RPP == 0 || M::row(tid, p) < ROWS);
-      this->r[p] = in ? load_chunk<Tag, VEC>(base + j * stride, d0, D) : (u32x4){0, 0, 0, 0};
-      if (mask) seen[p] = in ? mask[j * mask_s] : 0;
+      const int n = first + M::row(tid, p), j = n < end ? n : end - 1;
+      if constexpr (VEC)
+        this->r[p] = *(const u32x4 *)(base + j * stride);
+      else
+        this->r[p] = load_chunk<Tag, VEC>(base + j * stride, d0, D);
     }
   }
-  __device__ void store_seen(char *tile, int tid, bool masked) {
-    if (masked) {
+  __device__ void hide(bool rows, uint64_t see, int D, int tid) {
+    if (rows) {
 #pragma unroll
       for (int p = 0; p < M::NP; ++p)
-        if (!seen[p]) this->r[p] = (u32x4){0, 0, 0, 0};
+        if (!((see >> (M::row(tid, p) & 63)) & 1)) this->r[p] = (u32x4){0, 0, 0, 0};
     }
-    this->store(tile, tid);
+    this->cut(D, tid);
   }
 };
 
@@ -323,12 +335,14 @@ __device__ inline float other_half_sum(float v) {
 }
 __device__ inline float exp2_(float v) { return __builtin_amdgcn_exp2f(v); }
 
-// Visibility of states first .. first + n - 1, bit by bit, alike in all lanes.
-__device__ inline uint64_t visible(const AttnArgs &a, int64_t b, int first, int n, int end, int lane) {
-  const int j = first + lane;
-  bool see = lane < n && j < end;
-  if (a.mask && see) see = a.mask[b * a.mask_b + j * a.mask_s] != 0;
-  return __ballot(see);
+// Visibility of the n <= 64 states from `first` on: the mask's byte of lane's
+// state is loaded ahead, like the rows, and the bits are formed when they are
+// needed, alike in all lanes.
+__device__ inline uint32_t load_sight(const uint8_t *mask, int64_t mask_s, int first, int n, int len, int lane) {
+  return mask && lane < n && first + lane < len ? mask[(first + lane) * mask_s] : 1;
+}
+__device__ inline uint64_t sight_bits(uint32_t sight, int first, int n, int len, int lane) {
+  return __ballot(lane < n && first + lane < len && sight);
 }
 
 // Workgroup `id` of `n` onto a unit of work such that each die (workgroups
@@ -348,21 +362,38 @@ __device__ inline int length_of(const AttnArgs &a, int64_t b) {
   return len;
 }
 
-// Row fragments of 32 rows of a group (second operand): lane l has chunks
-// 2 u + h of row r (nothing for r >= R).
+// The chunks 2 u + h of one row, zeros past D.  (D > DP - 32, so only the last
+// chunks can lie past it.)
 template <class Tag, int DP, bool VEC>
-__device__ inline void load_rows(const AttnArgs &a, const Tokens &t, int64_t b, int hk, int r, int lane, u32x4 *f) {
+__device__ inline void load_row(const char *row, int D, int lane, u32x4 *f) {
   using T = Tile<Tag, DP>;
   const int h = lane >> 5;
-  if (r < a.R) {
-    const int s = r / a.G, g = r - s * a.G;
-    const char *row = t.p + b * t.b + s * t.s + (int64_t)(hk * a.G + g) * t.h;
 #pragma unroll
-    for (int u = 0; u < T::NU; ++u) f[u] = load_chunk<Tag, VEC>(row, (2 * u + h) * T::CE, a.D);
-  } else {
-#pragma unroll
-    for (int u = 0; u < T::NU; ++u) f[u] = (u32x4){0, 0, 0, 0};
+  for (int u = 0; u < T::NU; ++u) {
+    const int d0 = (2 * u + h) * T::CE;
+    if constexpr (!VEC)
+      f[u] = load_chunk<Tag, VEC>(row, d0, D);
+    else if ((2 * u + 2) * T::CE <= DP - 32)
+      f[u] = *(const u32x4 *)(row + d0 * Tag::ES);
+    else
+      f[u] = *(const u32x4 *)(row + (d0 < D ? d0 : 0) * Tag::ES);
   }
+  if constexpr (VEC) {
+    if (D < DP) {
+#pragma unroll
+      for (int u = 0; u < T::NU; ++u)
+        if ((2 * u + 2) * T::CE > DP - 32 && (2 * u + h) * T::CE >= D) f[u] = (u32x4){0, 0, 0, 0};
+    }
+  }
+}
+
+// Row fragments of 32 rows of a group (second operand): lane l has chunks
+// 2 u + h of row r; rows from R on repeat the last one, in columns of results
+// that nobody reads.
+template <class Tag, int DP, bool VEC>
+__device__ inline void load_rows(const AttnArgs &a, const Tokens &t, int64_t b, int hk, int r, int lane, u32x4 *f) {
+  const int at = r < a.R ? r : a.R - 1, s = at / a.G, g = at - s * a.G;
+  load_row<Tag, DP, VEC>(t.p + b * t.b + s * t.s + (int64_t)(hk * a.G + g) * t.h, a.D, lane, f);
 }
 
 // Address of row r of a group in an output, or null past the last.
@@ -435,37 +466,40 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
   const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
   StateMover<Tag, DP, VEC, F::BN, 256> mk, mv;
+  uint32_t sight = 1;
   const int rowlane = T::rowlane(lane), collane = T::collane(lane);
 
   f32x16 acc[DT] = {};
   float top = -INFINITY, sum = 0.f;
   if (t1 > 0) {
-    mk.load(kb, a.k.s, 0, len, mask, a.mask_s, a.D, tid);
-    mv.load(vb, a.v.s, 0, len, mask, a.mask_s, a.D, tid);
+    mk.load(kb, a.k.s, 0, len, a.D, tid);
+    mv.load(vb, a.v.s, 0, len, a.D, tid);
+    sight = load_sight(mask, a.mask_s, 0, F::BN, len, lane);
   }
   for (int t = 0; t < t1; ++t) {
-    char *kt = smem + (t & 1) * 2 * F::TILE, *vt = kt + F::TILE;
-    mk.store_seen(kt, tid, mask != nullptr);
-    mv.store_seen(vt, tid, mask != nullptr);
+    const int kt = (t & 1) * 2 * F::TILE, vt = kt + F::TILE;
+    uint64_t see = ~(uint64_t)0;
+    if (mask || (t + 1) * F::BN > len) see = sight_bits(sight, t * F::BN, F::BN, len, lane);
+    mk.hide(mask != nullptr, see, a.D, tid);
+    mv.hide(mask != nullptr, see, a.D, tid);
+    mk.store(smem + kt, tid);
+    mv.store(smem + vt, tid);
     __syncthreads();
     if (t + 1 < t1) {
-      mk.load(kb, a.k.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, tid);
-      mv.load(vb, a.v.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, tid);
+      mk.load(kb, a.k.s, (t + 1) * F::BN, len, a.D, tid);
+      mv.load(vb, a.v.s, (t + 1) * F::BN, len, a.D, tid);
+      sight = load_sight(mask, a.mask_s, (t + 1) * F::BN, F::BN, len, lane);
     }
     f32x16 s[NB];
 #pragma unroll
-    for (int k = 0; k < NB; ++k) s[k] = rows_product<Tag, DP>(kt, rowlane, wk * F::KW + 32 * k, qf);
-    if (a.mask || (t + 1) * F::BN > len) {
-      constexpr uint64_t FULL = F::KW == 64 ? ~(uint64_t)0 : 0xffffffffu;
-      const uint64_t see = (visible(a, b, t * F::BN, F::BN, len, lane) >> (wk * F::KW)) & FULL;
-      if (see != FULL) {
+    for (int k = 0; k < NB; ++k) s[k] = rows_product<Tag, DP>(smem, kt + rowlane, wk * F::KW + 32 * k, qf);
+    if (see != ~(uint64_t)0) {
 #pragma unroll
-        for (int k = 0; k < NB; ++k) {
-          const uint32_t bits = (uint32_t)(see >> (32 * k)) >> (4 * h);
+      for (int k = 0; k < NB; ++k) {
+        const uint32_t bits = (uint32_t)(see >> (wk * F::KW + 32 * k)) >> (4 * h);
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (!((bits >> (8 * (i / 4) + i % 4)) & 1)) s[k][i] = -INFINITY;
-        }
+        for (int i = 0; i < 16; ++i)
+          if (!((bits >> (8 * (i / 4) + i % 4)) & 1)) s[k][i] = -INFINITY;
       }
     }
     float fix;
@@ -487,7 +521,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
       // Weights are rounded to the inputs' type for the second product; their
       // sum is taken before that, in float32.
       const Weights<Tag> w = to_weights<Tag>(s[k]);
-      cols_product<Tag, DP>(vt, collane, wk * F::KW + 32 * k, w, acc);
+      cols_product<Tag, DP>(smem, vt + collane, wk * F::KW + 32 * k, w, acc);
     }
   }
   sum = other_half_sum(sum);
@@ -552,21 +586,12 @@ struct FewShape {
   }
 };
 
-// Row fragments (first operand) of the 32 states from `first` on, zeros where
-// they are not visible.
+// Row fragments (first operand) of the 32 states from `first` on; those from
+// `len` on repeat the last one.
 template <class Tag, int DP, bool VEC>
-__device__ inline void load_states(const AttnArgs &a, const char *base, int64_t stride, const uint8_t *mask, int first,
-                                   int len, int lane, u32x4 *f) {
-  using T = Tile<Tag, DP>;
-  const int h = lane >> 5, j = first + (lane & 31);
-  const bool in = j < len;
-#pragma unroll
-  for (int u = 0; u < T::NU; ++u)
-    f[u] = in ? load_chunk<Tag, VEC>(base + j * stride, (2 * u + h) * T::CE, a.D) : (u32x4){0, 0, 0, 0};
-  if (mask && in && !mask[j * a.mask_s]) {
-#pragma unroll
-    for (int u = 0; u < T::NU; ++u) f[u] = (u32x4){0, 0, 0, 0};
-  }
+__device__ inline void load_states(const char *base, int64_t stride, int first, int len, int D, int lane, u32x4 *f) {
+  const int n = first + (lane & 31);
+  load_row<Tag, DP, VEC>(base + (n < len ? n : len - 1) * stride, D, lane, f);
 }
 
 template <class Tag, int DP, bool VEC>
@@ -595,25 +620,34 @@ __global__ __launch_bounds__(256, Tag::W16 || DP <= 64 ? 2 : 1) void attn_few_ke
   const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
   const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
   StateMover<Tag, DP, VEC, 32, 64> mv;
-  char *vt = smem + wave * F::TILE;
+  const int vt = wave * F::TILE;
+  uint32_t sight = 1;
   const int collane = T::collane(lane);
   f32x16 acc[DT] = {};
   float top = -INFINITY, sum = 0.f;
   int t = t0 + wave;
   if (t < t1) {
-    load_states<Tag, DP, VEC>(a, kb, a.k.s, mask, t * 32, len, lane, kf);
-    mv.load(vb, a.v.s, t * 32, len, mask, a.mask_s, a.D, lane);
+    load_states<Tag, DP, VEC>(kb, a.k.s, t * 32, len, a.D, lane, kf);
+    mv.load(vb, a.v.s, t * 32, len, a.D, lane);
+    sight = load_sight(mask, a.mask_s, t * 32, 32, len, lane);
   }
   load_rows<Tag, DP, VEC>(a, a.q, b, hk, rt * 32 + l31, lane, qf);
   for (; t < t1; t += 4) {
     f32x16 s = {};
 #pragma unroll
     for (int u = 0; u < T::NU; ++u) s = mma_chunk<Tag>(kf[u], qf[u], s);
-    if (t + 4 < t1) load_states<Tag, DP, VEC>(a, kb, a.k.s, mask, (t + 4) * 32, len, lane, kf);
-    mv.store_seen(vt, lane, mask != nullptr);
-    if (t + 4 < t1) mv.load(vb, a.v.s, (t + 4) * 32, len, mask, a.mask_s, a.D, lane);
-    if (a.mask || (t + 1) * 32 > len) {
-      const uint32_t bits = (uint32_t)visible(a, b, t * 32, 32, len, lane) >> (4 * h);
+    const bool more = t + 4 < t1;
+    if (more) load_states<Tag, DP, VEC>(kb, a.k.s, (t + 4) * 32, len, a.D, lane, kf);
+    uint32_t see = 0xffffffffu;
+    if (mask || (t + 1) * 32 > len) see = (uint32_t)sight_bits(sight, t * 32, 32, len, lane);
+    mv.hide(mask != nullptr, see, a.D, lane);
+    mv.store(smem + vt, lane);
+    if (more) {
+      mv.load(vb, a.v.s, (t + 4) * 32, len, a.D, lane);
+      sight = load_sight(mask, a.mask_s, (t + 4) * 32, 32, len, lane);
+    }
+    if (see != 0xffffffffu) {
+      const uint32_t bits = see >> (4 * h);
 #pragma unroll
       for (int i = 0; i < 16; ++i)
         if (!((bits >> (8 * (i / 4) + i % 4)) & 1)) s[i] = -INFINITY;
@@ -632,7 +666,7 @@ __global__ __launch_bounds__(256, Tag::W16 || DP <= 64 ? 2 : 1) void attn_few_ke
     }
     wave_lds_fence();
     const Weights<Tag> w = to_weights<Tag>(s);
-    cols_product<Tag, DP>(vt, collane, 0, w, acc);
+    cols_product<Tag, DP>(smem, vt + collane, 0, w, acc);
     wave_lds_fence();
   }
   sum = other_half_sum(sum);
@@ -784,32 +818,37 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs
   const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
   const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
   StateMover<Tag, DP, VEC, F::BN, 256> mk, mv;
+  uint32_t sight = 1;
   const int rowlane = T::rowlane(lane), collane = T::collane(lane);
   f32x16 acc[DT] = {};
   if (t1 > 0) {
-    mk.load(kb, a.k.s, 0, len, mask, a.mask_s, a.D, tid);
-    mv.load(vb, a.v.s, 0, len, mask, a.mask_s, a.D, tid);
+    mk.load(kb, a.k.s, 0, len, a.D, tid);
+    mv.load(vb, a.v.s, 0, len, a.D, tid);
+    sight = load_sight(mask, a.mask_s, 0, F::BN, len, lane);
   }
   for (int t = 0; t < t1; ++t) {
-    char *kt = smem + (t & 1) * 2 * F::TILE, *vt = kt + F::TILE;
-    mk.store_seen(kt, tid, mask != nullptr);
-    mv.store_seen(vt, tid, mask != nullptr);
+    const int kt = (t & 1) * 2 * F::TILE, vt = kt + F::TILE;
+    uint64_t see = ~(uint64_t)0;
+    if (mask || (t + 1) * F::BN > len) see = sight_bits(sight, t * F::BN, F::BN, len, lane);
+    mk.hide(mask != nullptr, see, a.D, tid);
+    mv.hide(mask != nullptr, see, a.D, tid);
+    mk.store(smem + kt, tid);
+    mv.store(smem + vt, tid);
     __syncthreads();
     if (t + 1 < t1) {
-      mk.load(kb, a.k.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, tid);
-      mv.load(vb, a.v.s, (t + 1) * F::BN, len, mask, a.mask_s, a.D, tid);
+      mk.load(kb, a.k.s, (t + 1) * F::BN, len, a.D, tid);
+      mv.load(vb, a.v.s, (t + 1) * F::BN, len, a.D, tid);
+      sight = load_sight(mask, a.mask_s, (t + 1) * F::BN, F::BN, len, lane);
     }
-    uint64_t see = ~(uint64_t)0;
-    if (a.mask || (t + 1) * F::BN > len) see = visible(a, b, t * F::BN, F::BN, len, lane) >> (wk * F::KW);
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
       const int base = wk * F::KW + 32 * k;
-      f32x16 s = rows_product<Tag, DP>(kt, rowlane, base, qf);
-      const f32x16 dp = rows_product<Tag, DP>(vt, rowlane, base, gf);
-      to_ds(&s, dp, a.c, st, (uint32_t)(see >> (32 * k)), h);
+      f32x16 s = rows_product<Tag, DP>(smem, kt + rowlane, base, qf);
+      const f32x16 dp = rows_product<Tag, DP>(smem, vt + rowlane, base, gf);
+      to_ds(&s, dp, a.c, st, (uint32_t)(see >> base), h);
       // ds is rounded to the inputs' type for its product
       const Weights<Tag> w = to_weights<Tag>(s);
-      cols_product<Tag, DP>(kt, collane, base, w, acc);
+      cols_product<Tag, DP>(smem, kt + collane, base, w, acc);
     }
   }
   __syncthreads();
@@ -869,31 +908,42 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_few_dq_kernel(Attn
   load_rows<Tag, DP, VEC>(a, a.q, b, hk, rt * 32 + l31, lane, qf);
   load_rows<Tag, DP, VEC>(a, a.dout, b, hk, rt * 32 + l31, lane, gf);
   const float2 st = row_stat<Tag, DP, VEC>(a, b, hk, rt * 32 + l31, lane, gf, split == 0 && wave == 0);
-  char *kt = smem + wave * F::TILE;
+  const int kt = wave * F::TILE;
+  uint32_t sight = 1;
   const int rowlane = T::rowlane(lane), collane = T::collane(lane);
   f32x16 acc[DT] = {};
   int t = t0 + wave;
   if (t < t1) {
-    load_states<Tag, DP, VEC>(a, kb, a.k.s, mask, t * 32, len, lane, kf);
-    load_states<Tag, DP, VEC>(a, vb, a.v.s, mask, t * 32, len, lane, vf);
+    load_states<Tag, DP, VEC>(kb, a.k.s, t * 32, len, a.D, lane, kf);
+    load_states<Tag, DP, VEC>(vb, a.v.s, t * 32, len, a.D, lane, vf);
+    sight = load_sight(mask, a.mask_s, t * 32, 32, len, lane);
   }
   for (; t < t1; t += 4) {
+    const bool more = t + 4 < t1;
+    uint32_t see = 0xffffffffu;
+    if (mask || (t + 1) * 32 > len) see = (uint32_t)sight_bits(sight, t * 32, 32, len, lane);
+    if (mask && !((see >> l31) & 1)) {
+#pragma unroll
+      for (int u = 0; u < T::NU; ++u) kf[u] = (u32x4){0, 0, 0, 0};
+    }
     f32x16 s = {}, dp = {};
 #pragma unroll
     for (int u = 0; u < T::NU; ++u) {
       s = mma_chunk<Tag>(kf[u], qf[u], s);
-      *(u32x4 *)(kt + (rowlane ^ (u << 5))) = kf[u];
+      *(u32x4 *)(smem + ((kt + rowlane) ^ (u << 5))) = kf[u];
     }
-    if (t + 4 < t1) load_states<Tag, DP, VEC>(a, kb, a.k.s, mask, (t + 4) * 32, len, lane, kf);
+    if (more) load_states<Tag, DP, VEC>(kb, a.k.s, (t + 4) * 32, len, a.D, lane, kf);
 #pragma unroll
     for (int u = 0; u < T::NU; ++u) dp = mma_chunk<Tag>(vf[u], gf[u], dp);
-    if (t + 4 < t1) load_states<Tag, DP, VEC>(a, vb, a.v.s, mask, (t + 4) * 32, len, lane, vf);
-    uint32_t seen = 0xffffffffu;
-    if (a.mask || (t + 1) * 32 > len) seen = (uint32_t)visible(a, b, t * 32, 32, len, lane);
-    to_ds(&s, dp, a.c, st, seen, h);
+    if (more) {
+      load_states<Tag, DP, VEC>(vb, a.v.s, (t + 4) * 32, len, a.D, lane, vf);
+      sight = load_sight(mask, a.mask_s, (t + 4) * 32, 32, len, lane);
+    }
+    // (what a hidden state's values make of dp is replaced by zero)
+    to_ds(&s, dp, a.c, st, see, h);
     wave_lds_fence();
     const Weights<Tag> w = to_weights<Tag>(s);
-    cols_product<Tag, DP>(kt, collane, 0, w, acc);
+    cols_product<Tag, DP>(smem, kt + collane, 0, w, acc);
     wave_lds_fence();
   }
   float *xo = (float *)smem;
@@ -939,19 +989,42 @@ struct DkvShape {
   static constexpr int LDS = STAT + 2 * 2 * BR * 4 > 4 * OUT ? STAT + 2 * 2 * BR * 4 : 4 * OUT;
 };
 
-// Rows first .. first + ROWS - 1 of a group.
+// Tiles of ROWS rows of a group, one after the other.  The query and head of a
+// thread's rows are carried along, so that only the first tile divides.  Rows
+// from R on repeat the last one: their weights are zero.
 template <class Tag, int DP, bool VEC, int ROWS>
-struct RowMover : Mover<Tag, DP, ROWS, 256> {
+struct RowWalk {
   using M = Mover<Tag, DP, ROWS, 256>;
-  __device__ void load(const AttnArgs &a, const Tokens &t, int64_t b, int hk, int first, int end, int tid) {
-    const int d0 = M::chunk(tid) * M::T::CE;
+  int s[M::NP], g[M::NP], step_s, step_g;
+  __device__ void start(const AttnArgs &a, int first, int tid) {
+    step_s = ROWS / a.G;
+    step_g = ROWS - step_s * a.G;
 #pragma unroll
     for (int p = 0; p < M::NP; ++p) {
       const int r = first + M::row(tid, p);
-      this->r[p] = (u32x4){0, 0, 0, 0};
-      if (r < end && (ROWS % M::RPP == 0 || M::row(tid, p) < ROWS)) {
-        const int s = r / a.G, g = r - s * a.G;
-        this->r[p] = load_chunk<Tag, VEC>(t.p + b * t.b + s * t.s + (int64_t)(hk * a.G + g) * t.h, d0, a.D);
+      s[p] = r / a.G;
+      g[p] = r - s[p] * a.G;
+    }
+  }
+  __device__ void load(const AttnArgs &a, const char *qb, const char *gb, int tid, M *mq, M *mg) {
+    const int d0 = M::chunk(tid) * M::T::CE, dc = VEC ? (d0 < a.D ? d0 : 0) * Tag::ES : 0;
+#pragma unroll
+    for (int p = 0; p < M::NP; ++p) {
+      const bool in = s[p] < a.Sq;
+      const int sp = in ? s[p] : a.Sq - 1, gp = in ? g[p] : a.G - 1;
+      const char *q = qb + sp * a.q.s + gp * a.q.h + dc, *o = gb + sp * a.dout.s + gp * a.dout.h + dc;
+      if constexpr (VEC) {
+        mq->r[p] = *(const u32x4 *)q;
+        mg->r[p] = *(const u32x4 *)o;
+      } else {
+        mq->r[p] = load_chunk<Tag, VEC>(q, d0, a.D);
+        mg->r[p] = load_chunk<Tag, VEC>(o, d0, a.D);
+      }
+      s[p] += step_s;
+      g[p] += step_g;
+      if (g[p] >= a.G) {
+        g[p] -= a.G;
+        ++s[p];
       }
     }
   }
@@ -980,52 +1053,50 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
   int t1 = (int)((int64_t)all * (part + 1) / a.row_parts);
   if (kt0 * 128 >= len) t1 = t0;  // no state of the tile is visible
 
-  bool see = j < len;
-  if (a.mask && see) see = a.mask[b * a.mask_b + j * a.mask_s] != 0;
-  u32x4 kf[T::NU], vf[F::VLDS ? 1 : T::NU];
+  const bool see = j < len && (!a.mask || a.mask[b * a.mask_b + j * a.mask_s]);
+  u32x4 kf[T::NU], vf[T::NU];
   const int rowlane = T::rowlane(lane), collane = T::collane(lane);
-  char *const val = smem + F::VAL + wave * 32 * T::PITCH;  // this wave's values
-  {
-    const char *kr = a.k.p + b * a.k.b + hk * a.k.h + j * a.k.s, *vr = a.v.p + b * a.v.b + hk * a.v.h + j * a.v.s;
+  const int val = F::VAL + wave * 32 * T::PITCH + rowlane;  // this wave's values
+  // (a hidden state's column of results is its own, and is replaced by zeros)
+  load_states<Tag, DP, VEC>(a.k.p + b * a.k.b + hk * a.k.h, a.k.s, j0, a.Sk, a.D, lane, kf);
+  load_states<Tag, DP, VEC>(a.v.p + b * a.v.b + hk * a.v.h, a.v.s, j0, a.Sk, a.D, lane, vf);
+  if constexpr (F::VLDS) {
 #pragma unroll
-    for (int u = 0; u < T::NU; ++u) {
-      const int d0 = (2 * u + h) * T::CE;
-      kf[u] = see ? load_chunk<Tag, VEC>(kr, d0, a.D) : (u32x4){0, 0, 0, 0};
-      const u32x4 v = see ? load_chunk<Tag, VEC>(vr, d0, a.D) : (u32x4){0, 0, 0, 0};
-      if constexpr (F::VLDS)
-        *(u32x4 *)(val + (rowlane ^ (u << 5))) = v;
-      else
-        vf[u] = v;
-    }
+    for (int u = 0; u < T::NU; ++u) *(u32x4 *)(smem + (val ^ (u << 5))) = vf[u];
   }
-  RowMover<Tag, DP, VEC, F::BR> mq, mg;
+  Mover<Tag, DP, F::BR, 256> mq, mg;
+  RowWalk<Tag, DP, VEC, F::BR> walk;
+  const char *qb = a.q.p + b * a.q.b + (int64_t)hk * a.G * a.q.h, *gb = a.dout.p + b * a.dout.b + (int64_t)hk * a.G * a.dout.h;
+  walk.start(a, t0 * F::BR, tid);
   float2 st = make_float2(INFINITY, 0.f);
   auto load = [&](int t) {
-    mq.load(a, a.q, b, hk, t * F::BR, a.R, tid);
-    mg.load(a, a.dout, b, hk, t * F::BR, a.R, tid);
+    walk.load(a, qb, gb, tid, &mq, &mg);
     if (tid < F::BR) st = t * F::BR + tid < a.R ? a.rowstat[bh * a.R + t * F::BR + tid] : make_float2(INFINITY, 0.f);
   };
   f32x16 dk[DT] = {}, dv[DT] = {};
   if (t0 < t1) load(t0);
   for (int t = t0; t < t1; ++t) {
-    char *qt = smem + (t & 1) * 2 * F::TILE, *gt = qt + F::TILE;
+    const int qt = (t & 1) * 2 * F::TILE, gt = qt + F::TILE;
     float *stat = (float *)(smem + F::STAT) + (t & 1) * 2 * F::BR;
-    mq.store(qt, tid);
-    mg.store(gt, tid);
+    mq.cut(a.D, tid);
+    mg.cut(a.D, tid);
+    mq.store(smem + qt, tid);
+    mg.store(smem + gt, tid);
     if (tid < F::BR) {
       stat[tid] = st.x;
       stat[F::BR + tid] = st.y;
     }
     __syncthreads();
     if (t + 1 < t1) load(t + 1);
-    f32x16 s = rows_product<Tag, DP>(qt, rowlane, 0, kf);
+    f32x16 s = rows_product<Tag, DP>(smem, qt + rowlane, 0, kf);
     f32x16 dp = {};
     if constexpr (F::VLDS) {
 #pragma unroll
       for (int u = 0; u < T::NU; ++u)
-        dp = mma_chunk<Tag>(*(const u32x4 *)(gt + (rowlane ^ (u << 5))), *(const u32x4 *)(val + (rowlane ^ (u << 5))), dp);
+        dp = mma_chunk<Tag>(*(const u32x4 *)(smem + ((gt + rowlane) ^ (u << 5))), *(const u32x4 *)(smem + (val ^ (u << 5))),
+                            dp);
     } else {
-      dp = rows_product<Tag, DP>(gt, rowlane, 0, vf);
+      dp = rows_product<Tag, DP>(smem, gt + rowlane, 0, vf);
     }
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
@@ -1039,9 +1110,9 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
     }
     // p and ds are rounded to the inputs' type for their products
     const Weights<Tag> wp = to_weights<Tag>(s);
-    cols_product<Tag, DP>(gt, collane, 0, wp, dv);
+    cols_product<Tag, DP>(smem, gt + collane, 0, wp, dv);
     const Weights<Tag> wd = to_weights<Tag>(dp);
-    cols_product<Tag, DP>(qt, collane, 0, wd, dk);
+    cols_product<Tag, DP>(smem, qt + collane, 0, wd, dk);
   }
   if (!see) {
     // a state that is not visible has its column of results to itself
