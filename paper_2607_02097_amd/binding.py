@@ -604,8 +604,10 @@ def wbmm_hier(x, table_g, table_l, wl):
 # wbmm_rotary_args and wbmm_cross_attention_args of include/wbmm.h
 _ROTARY_ARGS = struct.Struct("25q")
 _ATTENTION_ARGS = struct.Struct("43qd3q")
-_NO_TOKENS = (0, 0, 0, 0)
+_NO_GRADIENTS = (0,) * 16
 MAX_AXES = 4
+_PAD = (0,) * MAX_AXES
+_POSITION_BYTES = {torch.int32: 4, torch.int64: 8}
 
 
 def _tokens(t: torch.Tensor, name: str):
@@ -615,29 +617,32 @@ def _tokens(t: torch.Tensor, name: str):
         raise TypeError("%s must be a torch.Tensor" % name)
     if not t.is_cuda:
         raise ValueError("%s must be a GPU tensor (got %s)" % (name, t.device))
-    if t.dim() != 4:
+    st = t.stride()
+    if len(st) != 4:
         raise ValueError("%s must be [B, S, H, D]" % name)
-    b, s, h, d = t.stride()
-    if d != 1 and t.shape[3] > 1:
+    if st[3] != 1 and t.shape[3] > 1:
         raise ValueError("%s: the components of a head must be contiguous" % name)
-    return t.data_ptr(), b, s, h
+    return t.data_ptr(), st[0], st[1], st[2]
 
 
-def _empty(shape, dtype, device, stream):
-    """A new tensor that belongs to the stream the call is enqueued on."""
+def _empty(like, shape, dtype, stream):
+    """A new tensor on ``like``'s device that belongs to the stream the call
+    is enqueued on."""
     if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(_torch_stream(device, stream)):
-        return torch.empty(shape, dtype=dtype, device=device)
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(_torch_stream(like.device, stream)):
+        return like.new_empty(shape, dtype=dtype)
 
 
-def _out_like(t, out, name, stream):
+def _out_like(t, shape, out, name, stream):
     """The output tensor of t's shape (new unless given) and its tokens."""
     if out is None:
-        out = _empty(t.shape, t.dtype, t.device, stream)
+        out = _empty(t, shape, t.dtype, stream)
+        B, S, H, D = shape
+        return out, (out.data_ptr(), S * H * D, H * D, D)
     tokens = _tokens(out, name)
-    if out.shape != t.shape or not _alike(out, t):
-        raise ValueError("%s must be %s in the inputs' dtype and device" % (name, list(t.shape)))
+    if out.shape != shape or not _alike(out, t):
+        raise ValueError("%s must be %s in the inputs' dtype and device" % (name, list(shape)))
     return out, tokens
 
 
@@ -654,16 +659,17 @@ def wbmm_rotary_frequencies(sections, base: float = 10000.0, restart: bool = Fal
 
 def _rotary_like(fn_name, x, positions, freqs, sections, adjacent, out, stream):
     xt = _tokens(x, "input")
-    B, S, H, D = x.shape
-    n = len(sections)
+    shape = x.shape
+    B, S, H, D = shape
+    n, index = len(sections), x.get_device()
     if not 1 <= n <= MAX_AXES:
         raise ValueError("sections must name 1 to %d axes" % MAX_AXES)
     for t, name in ((positions, "positions"), (freqs, "freqs")):
         if not isinstance(t, torch.Tensor):
             raise TypeError("%s must be a torch.Tensor" % name)
-        if t.get_device() != x.get_device():
+        if t.get_device() != index:
             raise ValueError("%s must be on the input's device" % name)
-    if positions.dtype not in (torch.int32, torch.int64):
+    if positions.dtype not in _POSITION_BYTES:
         raise TypeError("positions must be int32 or int64")
     if positions.shape != (n, B, S):
         raise ValueError("positions must be [axes, B, S] = %s" % [n, B, S])
@@ -671,11 +677,11 @@ def _rotary_like(fn_name, x, positions, freqs, sections, adjacent, out, stream):
         raise TypeError("freqs must be float32")
     if freqs.shape != (sum(sections),) or not freqs.is_contiguous():
         raise ValueError("freqs must be contiguous, one value a pair of sections")
-    out, yt = _out_like(x, out, "out", stream)
-    args = _ROTARY_ARGS.pack(*xt, *yt, positions.data_ptr(), positions.element_size(), *positions.stride(),
-                             freqs.data_ptr(), n, *sections, *(0,) * (MAX_AXES - n), 1 if adjacent else 0, B, S, H, D,
-                             _code(x.dtype))
-    _call(fn_name, x.get_device(), args, _stream(x, stream))
+    code = _code(x.dtype)
+    out, yt = _out_like(x, shape, out, "out", stream)
+    args = _ROTARY_ARGS.pack(*xt, *yt, positions.data_ptr(), _POSITION_BYTES[positions.dtype], *positions.stride(),
+                             freqs.data_ptr(), n, *sections, *_PAD[n:], 1 if adjacent else 0, B, S, H, D, code)
+    _call(fn_name, index, args, _stream(x, stream))
     return out
 
 
@@ -696,11 +702,12 @@ def wbmm_rotary_backward(dy, positions, freqs, sections, adjacent: bool = False,
 
 def _attention_sizes(q, k, v, kv_lens, key_mask, scale):
     """Checks the inputs; returns their tokens, the addresses and strides of
-    lengths and mask, sizes and scale."""
+    lengths and mask, and sizes, scale and type."""
     qt, kt, vt = _tokens(q, "q"), _tokens(k, "k"), _tokens(v, "v")
     B, Sq, Hq, D = q.shape
-    Sk, Hk = k.shape[1], k.shape[2]
-    if k.shape != (B, Sk, Hk, D) or v.shape != k.shape:
+    shape = k.shape
+    Bk, Sk, Hk, Dk = shape
+    if Bk != B or Dk != D or v.shape != shape:
         raise ValueError("k and v must be [B, Sk, Hk, D] with q's B and D")
     if Hk == 0 or Hq % Hk != 0:
         raise ValueError("q's heads must be a multiple of k's")
@@ -724,14 +731,20 @@ def _attention_sizes(q, k, v, kv_lens, key_mask, scale):
     return (*qt, *kt, *vt), (lens, mask, mask_b, mask_s, B, Sq, Sk, Hq, Hk, D, scale, _code(q.dtype))
 
 
-def _attention_call(way, q, pack, stream):
-    """The library call, with a workspace of its own where it needs one:
-    pack(address, bytes) gives the argument struct."""
-    lib = _lib if _lib is not None else load_library()
-    need = getattr(lib, "wbmm_cross_attention_%s_workspace_bytes" % way)(pack(0, 0))
-    # (freed on return, for later work of the same stream)
-    ws = _empty(need, torch.uint8, q.device, stream) if need else None
-    _call("wbmm_cross_attention_" + way, q.get_device(), pack(ws.data_ptr() if need else 0, need), _stream(q, stream))
+@functools.lru_cache(maxsize=1024)
+def _attention_workspace_bytes(fn_name, *sizes) -> int:
+    """A workspace query of the library (a function of sizes and type)."""
+    args = _ATTENTION_ARGS.pack(*(0,) * 37, *sizes[:6], 1.0, sizes[6], 0, 0)
+    return int(getattr(load_library(), fn_name)(args))
+
+
+def _attention_call(fn_name, q, tensors, lse, side, stream):
+    """The library call, with a workspace of its own where it needs one."""
+    need = _attention_workspace_bytes(fn_name + "_workspace_bytes", *side[4:10], side[11])
+    # (a workspace is freed on return, for later work of the same stream)
+    ws = _empty(q, need, torch.uint8, stream) if need else None
+    args = _ATTENTION_ARGS.pack(*tensors, lse, *side, ws.data_ptr() if need else 0, need)
+    _call(fn_name, q.get_device(), args, _stream(q, stream))
 
 
 def wbmm_cross_attention_forward(q, k, v, kv_lens=None, key_mask=None, scale=None, need_lse: bool = True, out=None,
@@ -743,13 +756,14 @@ def wbmm_cross_attention_forward(q, k, v, kv_lens=None, key_mask=None, scale=Non
     ``key_mask`` [B,Sk] (bool, true: visible) does not hide; a query that sees
     none gets zeros and minus infinity.  ``scale`` of the scores: D ** -0.5
     unless given."""
-    tokens, sizes = _attention_sizes(q, k, v, kv_lens, key_mask, scale)
-    out, ot = _out_like(q, out, "out", stream)
-    B, Sq, Hq, _ = q.shape
-    lse = _empty((B, Hq, Sq), torch.float32, q.device, stream) if need_lse else None
-    lse_ptr = lse.data_ptr() if need_lse else 0
-    _attention_call("forward", q, lambda ws, n: _ATTENTION_ARGS.pack(*tokens, *ot, *_NO_TOKENS * 4, lse_ptr, *sizes, ws,
-                                                                     n), stream)
+    tokens, side = _attention_sizes(q, k, v, kv_lens, key_mask, scale)
+    shape = q.shape
+    out, ot = _out_like(q, shape, out, "out", stream)
+    lse, lse_ptr = None, 0
+    if need_lse:
+        lse = _empty(q, (shape[0], shape[2], shape[1]), torch.float32, stream)
+        lse_ptr = lse.data_ptr()
+    _attention_call("wbmm_cross_attention_forward", q, (*tokens, *ot, *_NO_GRADIENTS), lse_ptr, side, stream)
     return out, lse
 
 
@@ -758,21 +772,20 @@ def wbmm_cross_attention_backward(dout, q, k, v, out, lse, kv_lens=None, key_mas
     """(dq, dk, dv) for upstream gradient dout, with the forward's inputs and
     its results out and lse.  Gradients of states that are not visible are
     zero."""
-    tokens, sizes = _attention_sizes(q, k, v, kv_lens, key_mask, scale)
-    B, Sq, Hq, _ = q.shape
+    tokens, side = _attention_sizes(q, k, v, kv_lens, key_mask, scale)
+    shape = q.shape
     ot, gt = _tokens(out, "out"), _tokens(dout, "dout")
     for t, name in ((out, "out"), (dout, "dout")):
-        if t.shape != q.shape or not _alike(t, q):
+        if t.shape != shape or not _alike(t, q):
             raise ValueError("%s must match q's shape, dtype and device" % name)
     _check_tensor(lse, "lse")
-    if lse.dtype != torch.float32 or lse.shape != (B, Hq, Sq) or lse.get_device() != q.get_device():
+    if lse.dtype != torch.float32 or lse.shape != (shape[0], shape[2], shape[1]) or lse.get_device() != q.get_device():
         raise ValueError("lse must be float32 [B, Hq, Sq] on q's device")
-    dq, dqt = _out_like(q, dq, "dq", stream)
-    dk, dkt = _out_like(k, dk, "dk", stream)
-    dv, dvt = _out_like(v, dv, "dv", stream)
-    lse_ptr = lse.data_ptr()
-    _attention_call("backward", q, lambda ws, n: _ATTENTION_ARGS.pack(*tokens, *ot, *gt, *dqt, *dkt, *dvt, lse_ptr,
-                                                                      *sizes, ws, n), stream)
+    dq, dqt = _out_like(q, shape, dq, "dq", stream)
+    dk, dkt = _out_like(k, k.shape, dk, "dk", stream)
+    dv, dvt = _out_like(v, k.shape, dv, "dv", stream)
+    _attention_call("wbmm_cross_attention_backward", q, (*tokens, *ot, *gt, *dqt, *dkt, *dvt), lse.data_ptr(), side,
+                    stream)
     return dq, dk, dv
 
 

@@ -717,7 +717,8 @@ __global__ __launch_bounds__(256, Tag::W16 || DP <= 64 ? 2 : 1) void attn_few_ke
 }
 
 // Joins the partial results of the splits, weighted by their shares of the
-// sum, in their order.  A thread takes one component of one row.
+// sum, in their order.  A thread takes one component of one row; the loads of
+// eight splits leave together.
 template <class Tag>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   const int64_t n = a.B * a.Hk * (int64_t)a.R;
@@ -725,14 +726,28 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
   if (e >= n * a.D) return;
   const int64_t row = e / a.D;
   const int d = (int)(e - row * a.D);
-  float top = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_l[s * n + row]);
-  float sum = 0.f, o = 0.f;
-  for (int s = 0; s < a.splits; ++s) {
-    const float l = a.part_l[s * n + row];
-    const float w = top == -INFINITY ? (l != l ? l : 0.f) : exp2_(l - top);
-    sum += w;
-    o += w * a.part_o[(s * n + row) * a.D + d];
+  float top = -INFINITY, sum = 0.f, o = 0.f;
+  for (int s0 = 0; s0 < a.splits; s0 += 8) {
+    float l[8], p[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int s = s0 + i < a.splits ? s0 + i : a.splits - 1;
+      l[i] = a.part_l[s * n + row];
+      p[i] = a.part_o[(s * n + row) * a.D + d];
+    }
+    float t = top;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t = fmaxf(t, l[i]);
+    const float sub = t == -INFINITY ? 0.f : t, fix = exp2_(top - sub);
+    sum *= fix;
+    o *= fix;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float w = s0 + i < a.splits ? exp2_(l[i] - sub) : 0.f;
+      sum += w;
+      o += w * p[i];
+    }
+    top = t;
   }
   o = sum == 0.f ? 0.f : o / sum;
   const int64_t bh = row / a.R, b = bh / a.Hk;
@@ -1151,7 +1166,13 @@ __global__ __launch_bounds__(256) void attn_sum_kernel(SumArgs a) {
   const float *part = a.part[blockIdx.y];
   const Tokens &t = a.out[blockIdx.y];
   float sum = 0.f;
-  for (int p = 0; p < a.parts; ++p) sum += part[p * n + e];
+  for (int p0 = 0; p0 < a.parts; p0 += 8) {
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = p0 + i < a.parts ? part[(p0 + i) * n + e] : 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += v[i];
+  }
   const int64_t row = e / a.D, bh = row / a.N, b = bh / a.Hk;
   const int d = (int)(e - row * a.D), r = (int)(row - bh * a.N), hk = (int)(bh - b * a.Hk);
   const int s = r / a.G, g = r - s * a.G;

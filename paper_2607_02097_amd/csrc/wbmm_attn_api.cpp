@@ -323,26 +323,37 @@ namespace wbmm {
 
 namespace {
 
-constexpr int64_t kUnits = 256;  // compute units; two workgroups fit each
+constexpr int64_t kUnits = 256;  // compute units
 
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t clamp(int64_t n, int64_t lo, int64_t hi) { return n < lo ? lo : n > hi ? hi : n; }
 
-// Tiles of 128 rows run the matrix cores best, but want one for each compute
-// unit; below that, tiles of 32 rows whose states go in parts, as many as
-// give two workgroups a unit, of at least eight blocks (two a wave).
+// Larger tiles of rows read the states less often and feed the matrix cores
+// better, but need a workgroup for three compute units in four: measured,
+// bfloat16, 128 / 64 / 32 rows: 192 heads of 100 rows 18.5 / 19.7 / 23.5 us
+// (192 workgroups of 128 rows), 32 heads of 512 rows 24 / 20 / 27 us (128), 16
+// heads of 512 rows over 3136 states 56 / 43 / 23 us (64).
+// Tiles of 32 rows can take the states in parts, for a workgroup on every
+// compute unit (one unit reads about 50 GB/s, whatever its waves), of 96 states
+// at least, since the parts are joined by a launch of its own; single tokens
+// over long sequences in up to eight workgroups a unit, so that unequal lengths
+// even out.  One token, 8 key heads of 128 components: 196 states 6.4 us in one
+// part, 8.1 in two; 784 states 11.7 us in one part, 9.1 in four, 8.2 in eight;
+// 12544 states 129 us in one, 25 in 8, 17 in 24 to 32.  32 tokens over 12544
+// states each: 294 us in one part, 285 in eight, 306 in 32.
 void plan_rows(AttnArgs *a) {
-  const int64_t bh = a->B * a->Hk;
+  const int64_t bh = a->B * a->Hk, enough = kUnits * 3 / 4;
   a->splits = 1;
-  if (a->R <= 64 && a->R > 32 && bh >= kUnits) {
-    a->tile_rows = 64;
-  } else if (a->R > 32 && bh * cdiv(a->R, 128) >= kUnits) {
+  if (a->R > 64 && bh * cdiv(a->R, 128) >= enough) {
     a->tile_rows = 128;
+  } else if (a->R > 32 && bh * cdiv(a->R, 64) >= enough) {
+    a->tile_rows = 64;
   } else {
     a->tile_rows = 32;
-    const int64_t wgs = bh * cdiv(a->R, 32), most = a->Sk / 256;
-    int64_t n = wgs > 0 ? 2 * kUnits / wgs : 1;
-    n = n < most ? n : most;
-    a->splits = n < 1 ? 1 : (int)n;
+    const int64_t wgs = bh * cdiv(a->R, 32);
+    int64_t n = wgs > 0 ? kUnits / wgs : 1;
+    if (a->R <= 32 && wgs > 0) n = n > a->Sk / 1536 ? n : clamp(8 * kUnits / wgs, 1, a->Sk / 1536);
+    a->splits = a->Sk > 384 ? (int)clamp(n, 1, clamp(a->Sk / 96, 1, 64)) : 1;
   }
 }
 
@@ -353,13 +364,15 @@ void attn_plan_forward(Dt, AttnArgs *a) {
   a->row_parts = 1;
 }
 
-void attn_plan_backward(Dt, AttnArgs *a) {
+// dk and dv: the rows in parts only where the states' tiles leave most of the
+// chip idle, of at least 512 rows (float32, whose products take sixteen times
+// as long: 128), since the parts are summed by a launch of its own: one key
+// head of 16384 rows and 64 states takes 402 us in one part and 37 in 32, 8 heads
+// of 256 rows and 784 states 40 us in one and 47 in two.
+void attn_plan_backward(Dt dt, AttnArgs *a) {
   plan_rows(a);
-  // dk, dv: parts of the rows until the chip is full, of at least four tiles
-  const int64_t wgs = a->B * a->Hk * cdiv(a->Sk, 128), most = a->R / 128;
-  int64_t n = wgs > 0 ? 2 * kUnits / wgs : 1;
-  n = n < most ? n : most;
-  a->row_parts = n < 1 ? 1 : (int)n;
+  const int64_t wgs = a->B * a->Hk * cdiv(a->Sk, 128);
+  a->row_parts = (int)clamp(wgs > 0 ? kUnits / wgs : 1, 1, clamp(a->R / (dt == Dt::F32 ? 128 : 512), 1, 64));
 }
 
 }  // namespace wbmm
