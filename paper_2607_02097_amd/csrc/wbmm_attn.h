@@ -54,6 +54,12 @@ struct Tile {
   static constexpr int LPC = PITCH / 16;                          // chunks of an LDS row
   static constexpr int NU = DP / (2 * CE);                        // chunk pairs of a row
   static constexpr int DT = DP / 32;
+  // The chunk of a row that belongs at a slot, for a load of whole rows (slots
+  // past the row, which nobody reads, take its first chunk).
+  __device__ static int chunk_at(int slot, int row) {
+    const int c = slot ^ swz(row);
+    return DP * ES < PITCH && c >= DP / CE ? 0 : c;
+  }
   __device__ static int swz(int row) {
     if constexpr (ES == 2) {
       if constexpr (PITCH == 256) return ((row & 3) << 2) | ((row >> 2) & 3);
@@ -323,6 +329,46 @@ struct StateMover : Mover<Tag, DP, ROWS, THREADS> {
   }
 };
 
+// ----------------------------------------------- from memory straight to LDS
+//
+// Tiles whose rows are all visible and whole (no mask, D = DP) skip the
+// registers: each lane names the 16 bytes that belong at its place in LDS, so
+// the swizzle is in the choice of the chunk.  This frees the registers of the
+// tile in flight (32 of 256 in the forward at 128 components).  Written as
+// assembly because the compiler, which cannot tell the two halves of the
+// double buffer apart, would wait for the loads of the next tile before each
+// read of the present one.  `lds` is the wave's first byte; lane l's piece goes
+// 16 l bytes behind it.
+__device__ inline void lds_load16(uint32_t lds, const char *base, uint32_t offset) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(offset), "s"(base) : "m0");
+}
+__device__ inline void lds_load16(uint32_t lds, const char *at) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(at) : "m0");
+}
+// The wave's loads have arrived (a barrier then tells the others).
+__device__ inline void lds_loads_done() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
+
+__device__ inline uint32_t lds_offset(const char *p) {
+  return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)p;
+}
+
+// A tile of ROWS states by four waves.  Strides are below 2^24 bytes (the
+// launcher checks), so a lane's offset in a tile fits 32 bits.
+template <class Tag, int DP, int ROWS>
+struct DirectStates {
+  using M = Mover<Tag, DP, ROWS, 256>;
+  static_assert(ROWS % M::RPP == 0, "whole passes");
+  __device__ static void load(uint32_t lds, const char *base, int64_t stride, int first, int end, int tid, int wave) {
+    const int c = M::chunk(tid);
+    const char *tile = base + first * stride;
+#pragma unroll
+    for (int p = 0; p < M::NP; ++p) {
+      const int rw = M::row(tid, p), last = end - 1 - first, j = rw < last ? rw : last;
+      lds_load16(lds + p * 4096 + wave * 1024, tile, (uint32_t)j * (uint32_t)stride + (M::T::chunk_at(c, rw) << 4));
+    }
+  }
+};
+
 __device__ inline float other_half_max(float v) {
   const auto r = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, v), __builtin_bit_cast(uint32_t, v), false,
                                                   false);
@@ -443,7 +489,7 @@ struct FwdShape {
   static constexpr int LDS = 4 * TILE;
 };
 
-template <class Tag, int DP, int WK, bool VEC>
+template <class Tag, int DP, int WK, bool VEC, bool DIRECT>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   using T = Tile<Tag, DP>;
   using F = FwdShape<Tag, DP, WK>;
@@ -464,32 +510,39 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   u32x4 qf[T::NU];
   load_rows<Tag, DP, VEC>(a, a.q, b, hk, r, lane, qf);
   const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
-  const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
+  const uint8_t *mask = !DIRECT && a.mask ? a.mask + b * a.mask_b : nullptr;
   StateMover<Tag, DP, VEC, F::BN, 256> mk, mv;
   uint32_t sight = 1;
   const int rowlane = T::rowlane(lane), collane = T::collane(lane);
 
   f32x16 acc[DT] = {};
   float top = -INFINITY, sum = 0.f;
-  if (t1 > 0) {
-    mk.load(kb, a.k.s, 0, len, a.D, tid);
-    mv.load(vb, a.v.s, 0, len, a.D, tid);
-    sight = load_sight(mask, a.mask_s, 0, F::BN, len, lane);
-  }
+  auto load = [&](int t) {
+    if constexpr (DIRECT) {
+      const uint32_t to = lds_offset(smem) + (t & 1) * 2 * F::TILE;
+      DirectStates<Tag, DP, F::BN>::load(to, kb, a.k.s, t * F::BN, len, tid, wave);
+      DirectStates<Tag, DP, F::BN>::load(to + F::TILE, vb, a.v.s, t * F::BN, len, tid, wave);
+    } else {
+      mk.load(kb, a.k.s, t * F::BN, len, a.D, tid);
+      mv.load(vb, a.v.s, t * F::BN, len, a.D, tid);
+      sight = load_sight(mask, a.mask_s, t * F::BN, F::BN, len, lane);
+    }
+  };
+  if (t1 > 0) load(0);
   for (int t = 0; t < t1; ++t) {
     const int kt = (t & 1) * 2 * F::TILE, vt = kt + F::TILE;
     uint64_t see = ~(uint64_t)0;
     if (mask || (t + 1) * F::BN > len) see = sight_bits(sight, t * F::BN, F::BN, len, lane);
-    mk.hide(mask != nullptr, see, a.D, tid);
-    mv.hide(mask != nullptr, see, a.D, tid);
-    mk.store(smem + kt, tid);
-    mv.store(smem + vt, tid);
-    __syncthreads();
-    if (t + 1 < t1) {
-      mk.load(kb, a.k.s, (t + 1) * F::BN, len, a.D, tid);
-      mv.load(vb, a.v.s, (t + 1) * F::BN, len, a.D, tid);
-      sight = load_sight(mask, a.mask_s, (t + 1) * F::BN, F::BN, len, lane);
+    if constexpr (DIRECT) {
+      lds_loads_done();
+    } else {
+      mk.hide(mask != nullptr, see, a.D, tid);
+      mv.hide(mask != nullptr, see, a.D, tid);
+      mk.store(smem + kt, tid);
+      mv.store(smem + vt, tid);
     }
+    __syncthreads();
+    if (t + 1 < t1) load(t + 1);
     f32x16 s[NB];
 #pragma unroll
     for (int k = 0; k < NB; ++k) s[k] = rows_product<Tag, DP>(smem, kt + rowlane, wk * F::KW + 32 * k, qf);
@@ -811,7 +864,7 @@ __device__ inline void to_ds(f32x16 *s, const f32x16 &dp, float c, float2 st, ui
 
 // dq: as the forward, a workgroup takes 32 (4 / WK) rows and runs over all
 // states, WK waves sharing rows and splitting each tile.
-template <class Tag, int DP, int WK, bool VEC>
+template <class Tag, int DP, int WK, bool VEC, bool DIRECT>
 __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs a) {
   using T = Tile<Tag, DP>;
   using F = FwdShape<Tag, DP, WK>;
@@ -831,30 +884,37 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs
   load_rows<Tag, DP, VEC>(a, a.dout, b, hk, r, lane, gf);
   const float2 st = row_stat<Tag, DP, VEC>(a, b, hk, r, lane, gf, wk == 0);
   const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
-  const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
+  const uint8_t *mask = !DIRECT && a.mask ? a.mask + b * a.mask_b : nullptr;
   StateMover<Tag, DP, VEC, F::BN, 256> mk, mv;
   uint32_t sight = 1;
   const int rowlane = T::rowlane(lane), collane = T::collane(lane);
   f32x16 acc[DT] = {};
-  if (t1 > 0) {
-    mk.load(kb, a.k.s, 0, len, a.D, tid);
-    mv.load(vb, a.v.s, 0, len, a.D, tid);
-    sight = load_sight(mask, a.mask_s, 0, F::BN, len, lane);
-  }
+  auto load = [&](int t) {
+    if constexpr (DIRECT) {
+      const uint32_t to = lds_offset(smem) + (t & 1) * 2 * F::TILE;
+      DirectStates<Tag, DP, F::BN>::load(to, kb, a.k.s, t * F::BN, len, tid, wave);
+      DirectStates<Tag, DP, F::BN>::load(to + F::TILE, vb, a.v.s, t * F::BN, len, tid, wave);
+    } else {
+      mk.load(kb, a.k.s, t * F::BN, len, a.D, tid);
+      mv.load(vb, a.v.s, t * F::BN, len, a.D, tid);
+      sight = load_sight(mask, a.mask_s, t * F::BN, F::BN, len, lane);
+    }
+  };
+  if (t1 > 0) load(0);
   for (int t = 0; t < t1; ++t) {
     const int kt = (t & 1) * 2 * F::TILE, vt = kt + F::TILE;
     uint64_t see = ~(uint64_t)0;
     if (mask || (t + 1) * F::BN > len) see = sight_bits(sight, t * F::BN, F::BN, len, lane);
-    mk.hide(mask != nullptr, see, a.D, tid);
-    mv.hide(mask != nullptr, see, a.D, tid);
-    mk.store(smem + kt, tid);
-    mv.store(smem + vt, tid);
-    __syncthreads();
-    if (t + 1 < t1) {
-      mk.load(kb, a.k.s, (t + 1) * F::BN, len, a.D, tid);
-      mv.load(vb, a.v.s, (t + 1) * F::BN, len, a.D, tid);
-      sight = load_sight(mask, a.mask_s, (t + 1) * F::BN, F::BN, len, lane);
+    if constexpr (DIRECT) {
+      lds_loads_done();
+    } else {
+      mk.hide(mask != nullptr, see, a.D, tid);
+      mv.hide(mask != nullptr, see, a.D, tid);
+      mk.store(smem + kt, tid);
+      mv.store(smem + vt, tid);
     }
+    __syncthreads();
+    if (t + 1 < t1) load(t + 1);
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
       const int base = wk * F::KW + 32 * k;
@@ -1021,14 +1081,24 @@ struct RowWalk {
       g[p] = r - s[p] * a.G;
     }
   }
-  __device__ void load(const AttnArgs &a, const char *qb, const char *gb, int tid, M *mq, M *mg) {
+  // To registers, or (DIRECT) to the tiles of LDS at `lds`.
+  template <bool DIRECT>
+  __device__ void load(const AttnArgs &a, const char *qb, const char *gb, int tid, M *mq, M *mg, uint32_t lds, int wave) {
     const int d0 = M::chunk(tid) * M::T::CE, dc = VEC ? (d0 < a.D ? d0 : 0) * Tag::ES : 0;
 #pragma unroll
     for (int p = 0; p < M::NP; ++p) {
       const bool in = s[p] < a.Sq;
       const int sp = in ? s[p] : a.Sq - 1, gp = in ? g[p] : a.G - 1;
-      const char *q = qb + sp * a.q.s + gp * a.q.h + dc, *o = gb + sp * a.dout.s + gp * a.dout.h + dc;
-      if constexpr (VEC) {
+      const char *q = qb + sp * a.q.s + gp * a.q.h, *o = gb + sp * a.dout.s + gp * a.dout.h;
+      if constexpr (!DIRECT) q += dc, o += dc;
+      if constexpr (DIRECT) {
+        const int c = M::T::chunk_at(M::chunk(tid), M::row(tid, p)) << 4;
+        const uint32_t to = lds + p * 4096 + wave * 1024;
+        if (ROWS % M::RPP == 0 || wave * (M::RPP / 4) < ROWS) {
+          lds_load16(to, q + c);
+          lds_load16(to + ROWS * M::T::PITCH, o + c);
+        }
+      } else if constexpr (VEC) {
         mq->r[p] = *(const u32x4 *)q;
         mg->r[p] = *(const u32x4 *)o;
       } else {
@@ -1045,7 +1115,7 @@ struct RowWalk {
   }
 };
 
-template <class Tag, int DP, bool VEC>
+template <class Tag, int DP, bool VEC, bool DIRECT>
 __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArgs a) {
   using T = Tile<Tag, DP>;
   using F = DkvShape<Tag, DP>;
@@ -1085,7 +1155,7 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
   walk.start(a, t0 * F::BR, tid);
   float2 st = make_float2(INFINITY, 0.f);
   auto load = [&](int t) {
-    walk.load(a, qb, gb, tid, &mq, &mg);
+    walk.template load<DIRECT>(a, qb, gb, tid, &mq, &mg, lds_offset(smem) + (t & 1) * 2 * F::TILE, wave);
     if (tid < F::BR) st = t * F::BR + tid < a.R ? a.rowstat[bh * a.R + t * F::BR + tid] : make_float2(INFINITY, 0.f);
   };
   f32x16 dk[DT] = {}, dv[DT] = {};
@@ -1093,10 +1163,14 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
   for (int t = t0; t < t1; ++t) {
     const int qt = (t & 1) * 2 * F::TILE, gt = qt + F::TILE;
     float *stat = (float *)(smem + F::STAT) + (t & 1) * 2 * F::BR;
-    mq.cut(a.D, tid);
-    mg.cut(a.D, tid);
-    mq.store(smem + qt, tid);
-    mg.store(smem + gt, tid);
+    if constexpr (DIRECT) {
+      lds_loads_done();
+    } else {
+      mq.cut(a.D, tid);
+      mg.cut(a.D, tid);
+      mq.store(smem + qt, tid);
+      mg.store(smem + gt, tid);
+    }
     if (tid < F::BR) {
       stat[tid] = st.x;
       stat[F::BR + tid] = st.y;
@@ -1192,6 +1266,12 @@ constexpr int64_t kMaxGrid = 1 << 23;  // workgroups of 256 threads in a launch
     if (e_ != hipSuccess) return e_;                                 \
   } while (0)
 
+// Tiles of states can go straight to LDS.
+template <class Tag, int DP, bool VEC>
+bool states_direct(const AttnArgs &a) {
+  return VEC && !a.mask && a.D == DP && a.k.s < (1 << 24) && a.v.s < (1 << 24);
+}
+
 template <class Tag, int DP, bool VEC>
 hipError_t launch_fwd(const AttnArgs &a, hipStream_t stream) {
   const int64_t bh = a.B * a.Hk;
@@ -1199,9 +1279,11 @@ hipError_t launch_fwd(const AttnArgs &a, hipStream_t stream) {
     WBMM_ATTN_LAUNCH((attn_few_kernel<Tag, DP, VEC>), bh * ((a.R + 31) / 32) * a.splits, (FewShape<Tag, DP>::lds(a.R)), a);
     if (a.splits > 1) WBMM_ATTN_LAUNCH((attn_join_kernel<Tag>), (bh * a.R * a.D + 255) / 256, 0, a);
   } else if (a.tile_rows == 64) {
-    WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 2, VEC>), bh * ((a.R + 63) / 64), (FwdShape<Tag, DP, 2>::LDS), a);
+    WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 2, VEC, false>), bh * ((a.R + 63) / 64), (FwdShape<Tag, DP, 2>::LDS), a);
+  } else if (states_direct<Tag, DP, VEC>(a)) {
+    WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 1, VEC, VEC>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
   } else {
-    WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 1, VEC>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
+    WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 1, VEC, false>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
   }
   return hipSuccess;
 }
@@ -1218,13 +1300,19 @@ hipError_t launch_bwd(const AttnArgs &a, hipStream_t stream) {
         WBMM_ATTN_LAUNCH((attn_sum_kernel<Tag>), (bh * a.R * a.D + 255) / 256, 0, s);
       }
     } else if (a.tile_rows == 64) {
-      WBMM_ATTN_LAUNCH((attn_dq_kernel<Tag, DP, 2, VEC>), bh * ((a.R + 63) / 64), (FwdShape<Tag, DP, 2>::LDS), a);
+      WBMM_ATTN_LAUNCH((attn_dq_kernel<Tag, DP, 2, VEC, false>), bh * ((a.R + 63) / 64), (FwdShape<Tag, DP, 2>::LDS), a);
+    } else if (states_direct<Tag, DP, VEC>(a)) {
+      WBMM_ATTN_LAUNCH((attn_dq_kernel<Tag, DP, 1, VEC, VEC>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
     } else {
-      WBMM_ATTN_LAUNCH((attn_dq_kernel<Tag, DP, 1, VEC>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
+      WBMM_ATTN_LAUNCH((attn_dq_kernel<Tag, DP, 1, VEC, false>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
     }
   }
   if (a.Sk == 0) return hipSuccess;
-  WBMM_ATTN_LAUNCH((attn_dkv_kernel<Tag, DP, VEC>), bh * ((a.Sk + 127) / 128) * a.row_parts, (DkvShape<Tag, DP>::LDS), a);
+  const int64_t n_dkv = bh * ((a.Sk + 127) / 128) * a.row_parts;
+  if (VEC && a.D == DP)
+    WBMM_ATTN_LAUNCH((attn_dkv_kernel<Tag, DP, VEC, VEC>), n_dkv, (DkvShape<Tag, DP>::LDS), a);
+  else
+    WBMM_ATTN_LAUNCH((attn_dkv_kernel<Tag, DP, VEC, false>), n_dkv, (DkvShape<Tag, DP>::LDS), a);
   if (a.row_parts > 1) {
     const SumArgs s = {{a.part_dk, a.part_dv}, {a.dk, a.dv}, bh * a.Sk, a.row_parts, a.Sk, 1, a.Hk, a.D};
     const int64_t n = (bh * a.Sk * a.D + 255) / 256;
