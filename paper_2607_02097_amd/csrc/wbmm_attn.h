@@ -126,15 +126,60 @@ template <class Tag> __device__ inline f32x16 mma_chunk(u32x4 a, u32x4 b, f32x16
 // rowlane().  (The tile is part of what the chunk's bits are xored into: the
 // address costs one instruction a read, and no registers between tiles.)
 template <class Tag, int DP>
-__device__ inline f32x16 rows_product(const char *smem, int at, int base, const u32x4 *b) {
+__device__ inline f32x16 rows_product(const char *smem, int at, int base, const u32x4 *b, f32x16 acc = {}) {
   using T = Tile<Tag, DP>;
-  f32x16 acc = {};
 #pragma unroll
   for (int u = 0; u < T::NU; ++u) {
     const u32x4 a = *(const u32x4 *)(smem + (at ^ (u << 5)) + base * T::PITCH);
     acc = mma_chunk<Tag>(a, b[u], acc);
   }
   return acc;
+}
+
+// Nothing is scheduled across this point.
+__device__ inline void pin_order() { __builtin_amdgcn_sched_barrier(0); }
+
+// As rows_product for NB blocks of 32 rows, with the reads P ahead of the
+// products (left to itself the compiler reads each fragment right before its
+// product and waits).
+template <class Tag, int DP, int NB, int P>
+__device__ inline void rows_products(const char *smem, int at, int base, const u32x4 *b, f32x16 *acc) {
+  using T = Tile<Tag, DP>;
+  constexpr int N = T::NU * NB;
+  constexpr int Q = P < N ? P : N;
+  u32x4 f[Q];
+  auto read = [&](int n) { return *(const u32x4 *)(smem + (at ^ ((n / NB) << 5)) + (base + 32 * (n % NB)) * T::PITCH); };
+#pragma unroll
+  for (int k = 0; k < NB; ++k) acc[k] = (f32x16){};
+#pragma unroll
+  for (int n = 0; n < Q; ++n) f[n] = read(n);
+  pin_order();
+#pragma unroll
+  for (int n = 0; n < N; ++n) {
+    acc[n % NB] = mma_chunk<Tag>(f[n % Q], b[n / NB], acc[n % NB]);
+    if (n + Q < N) f[n % Q] = read(n + Q);
+    pin_order();
+  }
+}
+
+// Column fragment dt of rows base .. base + 15 of an LDS tile (16-bit).
+template <class Tag, int DP>
+__device__ inline u32x4 col_read(const char *smem, int at, int base, int dt) {
+  using T = Tile<Tag, DP>;
+  s16x4 v[2];
+#pragma unroll
+  for (int g = 0; g < 2; ++g)
+    v[g] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (lds_s16x4 *)(smem + (at ^ (dt << 6) ^ (g << 5)) + (base + 8 * g) * T::PITCH));
+  const u32x2 lo = __builtin_bit_cast(u32x2, v[0]), hi = __builtin_bit_cast(u32x2, v[1]);
+  return (u32x4){lo[0], lo[1], hi[0], hi[1]};
+}
+
+// Column fragments of rows base .. base + 15 of an LDS tile.
+template <class Tag, int DP>
+__device__ inline void cols_read(const char *smem, int at, int base, u32x4 *f) {
+#pragma unroll
+  for (int dt = 0; dt < Tile<Tag, DP>::DT; ++dt) f[dt] = col_read<Tag, DP>(smem, at, base, dt);
 }
 
 // Second operand over 32 rows made of a lane's 16 results.
@@ -442,6 +487,14 @@ __device__ inline void load_rows(const AttnArgs &a, const Tokens &t, int64_t b, 
   load_row<Tag, DP, VEC>(t.p + b * t.b + s * t.s + (int64_t)(hk * a.G + g) * t.h, a.D, lane, f);
 }
 
+// The fragments have arrived.  (Loads still under way when a loop is entered
+// make the compiler wait inside it, every time round, and that wait would take
+// in the loads of the next tile.)
+template <int N> __device__ inline void arrived(u32x4 (&f)[N]) {
+#pragma unroll
+  for (int u = 0; u < N; ++u) asm volatile("" : "+v"(f[u]));
+}
+
 // Address of row r of a group in an output, or null past the last.
 __device__ inline char *group_row(const AttnArgs &a, const Tokens &t, int64_t b, int hk, int r) {
   if (r >= a.R) return nullptr;
@@ -529,6 +582,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
     }
   };
   if (t1 > 0) load(0);
+  arrived(qf);
   for (int t = 0; t < t1; ++t) {
     const int kt = (t & 1) * 2 * F::TILE, vt = kt + F::TILE;
     uint64_t see = ~(uint64_t)0;
@@ -544,8 +598,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
     __syncthreads();
     if (t + 1 < t1) load(t + 1);
     f32x16 s[NB];
-#pragma unroll
-    for (int k = 0; k < NB; ++k) s[k] = rows_product<Tag, DP>(smem, kt + rowlane, wk * F::KW + 32 * k, qf);
+    rows_products<Tag, DP, NB, Tag::W16 ? 8 : 4>(smem, kt + rowlane, wk * F::KW, qf, s);
     if (see != ~(uint64_t)0) {
 #pragma unroll
       for (int k = 0; k < NB; ++k) {
@@ -555,6 +608,11 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
           if (!((bits >> (8 * (i / 4) + i % 4)) & 1)) s[k][i] = -INFINITY;
       }
     }
+    u32x4 vf[2][DT];
+    if constexpr (Tag::W16) {
+      cols_read<Tag, DP>(smem, vt + collane, wk * F::KW, vf[0]);
+      pin_order();
+    }
     float fix;
     if (running_top<NB>(s, a.c, &top, &fix)) {
       sum *= fix;
@@ -562,19 +620,42 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
       for (int d = 0; d < DT; ++d) acc[d] *= fix;
     }
     const float sub = top == -INFINITY ? 0.f : top;
+    if constexpr (Tag::W16) {
+      // Eight weights at a time: those of the next step are formed while the
+      // matrix cores take this step's.  They are rounded to the inputs' type for
+      // the product; their sum is taken before that, in float32.
+      u32x4 w[2];
+      auto weights = [&](int n, u32x4 *to) {
+        float p[8];
 #pragma unroll
-    for (int k = 0; k < NB; ++k) {
-      float part[2] = {0.f, 0.f};
+        for (int i = 0; i < 8; ++i) p[i] = exp2_(__builtin_fmaf(s[n / 2][8 * (n & 1) + i], a.c, -sub));
+        sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[k][i] = exp2_(__builtin_fmaf(s[k][i], a.c, -sub));
-        part[i & 1] += s[k][i];
+        for (int j = 0; j < 4; ++j) (*to)[j] = pack2<Tag>(p[2 * j], p[2 * j + 1]);
+      };
+      weights(0, &w[0]);
+#pragma unroll
+      for (int n = 0; n < 2 * NB; ++n) {
+        if (n + 1 < 2 * NB) cols_read<Tag, DP>(smem, vt + collane, wk * F::KW + 16 * (n + 1), vf[(n + 1) & 1]);
+        pin_order();
+#pragma unroll
+        for (int d = 0; d < DT; ++d) acc[d] = mma_chunk<Tag>(vf[n & 1][d], w[n & 1], acc[d]);
+        if (n + 1 < 2 * NB) weights(n + 1, &w[(n + 1) & 1]);
+
+        pin_order();
       }
-      sum += part[0] + part[1];
-      // Weights are rounded to the inputs' type for the second product; their
-      // sum is taken before that, in float32.
-      const Weights<Tag> w = to_weights<Tag>(s[k]);
-      cols_product<Tag, DP>(smem, vt + collane, wk * F::KW + 32 * k, w, acc);
+    } else {
+#pragma unroll
+      for (int k = 0; k < NB; ++k) {
+        float part[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[k][i] = exp2_(__builtin_fmaf(s[k][i], a.c, -sub));
+          part[i & 1] += s[k][i];
+        }
+        sum += part[0] + part[1];
+        cols_product<Tag, DP>(smem, vt + collane, wk * F::KW + 32 * k, to_weights<Tag>(s[k]), acc);
+      }
     }
   }
   sum = other_half_sum(sum);
@@ -819,9 +900,10 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 // dq, states for dk and dv), so every sum has one owner and a fixed order: no
 // atomics, and the same bits every time.
 
-// Statistics of the lane's row: {lse in log2 units, delta}; a row that sees
-// nothing gets +infinity, so that its weights come out as zero.  Kept for the
-// kernel of dk and dv by one lane a row (`keep`).
+// What the products of the lane's row start from: {-lse / scale, -delta}, so
+// that they come out as the weight's exponent and as dp - delta; a row that
+// sees nothing starts from minus infinity, and its weights come out as zero.
+// Kept for the kernel of dk and dv by one lane a row (`keep`).
 template <class Tag, int DP, bool VEC>
 __device__ inline float2 row_stat(const AttnArgs &a, int64_t b, int hk, int r, int lane, const u32x4 *gf, bool keep) {
   using T = Tile<Tag, DP>;
@@ -840,20 +922,31 @@ __device__ inline float2 row_stat(const AttnArgs &a, int64_t b, int hk, int r, i
         d += __uint_as_float(x) * __uint_as_float(y);
     }
   d = other_half_sum(d);
-  float2 st = make_float2(INFINITY, 0.f);
+  float2 st = make_float2(-INFINITY, 0.f);
   if (r < a.R) {
     const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
     const float lse = a.lse[(b * a.Hq + hq) * a.Sq + sq];
-    if (lse != -INFINITY) st = make_float2(lse * kLog2e, d);
+    if (lse != -INFINITY) st = make_float2(-lse / a.scale, -d);
     if (keep && lane < 32) a.rowstat[(b * a.Hk + hk) * a.R + r] = st;
   }
   return st;
 }
 
-// Scores to ds (one lane: 16 states of one row), zero where not visible.
-__device__ inline void to_ds(f32x16 *s, const f32x16 &dp, float c, float2 st, uint32_t seen, int h) {
+// (The value is made anew each time: sixteen copies of it would otherwise be
+// kept in registers across a loop.)
+__device__ inline f32x16 splat(float v) {
+  asm volatile("" : "+v"(v));
+  f32x16 r;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) (*s)[i] = exp2_(__builtin_fmaf((*s)[i], c, -st.x)) * (dp[i] - st.y);
+  for (int i = 0; i < 16; ++i) r[i] = v;
+  return r;
+}
+
+// Exponents and dp - delta to ds (one lane: 16 states of one row), zero where
+// not visible.
+__device__ inline void to_ds(f32x16 *s, const f32x16 &dp, float c, uint32_t seen, int h) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i) (*s)[i] = exp2_((*s)[i] * c) * dp[i];
   if (seen != 0xffffffffu) {
     const uint32_t bits = seen >> (4 * h);
 #pragma unroll
@@ -901,6 +994,8 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs
     }
   };
   if (t1 > 0) load(0);
+  arrived(qf);
+  arrived(gf);
   for (int t = 0; t < t1; ++t) {
     const int kt = (t & 1) * 2 * F::TILE, vt = kt + F::TILE;
     uint64_t see = ~(uint64_t)0;
@@ -918,12 +1013,59 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
       const int base = wk * F::KW + 32 * k;
-      f32x16 s = rows_product<Tag, DP>(smem, kt + rowlane, base, qf);
-      const f32x16 dp = rows_product<Tag, DP>(smem, vt + rowlane, base, gf);
-      to_ds(&s, dp, a.c, st, (uint32_t)(see >> base), h);
-      // ds is rounded to the inputs' type for its product
-      const Weights<Tag> w = to_weights<Tag>(s);
-      cols_product<Tag, DP>(smem, kt + collane, base, w, acc);
+      f32x16 s = splat(st.x), dp = splat(st.y);
+      const uint32_t seen = (uint32_t)(see >> base);
+      if constexpr (Tag::W16 && DIRECT) {
+        // One stream of fragment reads, some products ahead of their use: keys
+        // for the scores, values for dp (while which the weights are formed),
+        // columns of the keys for dq.
+        constexpr int NU = T::NU, N = 2 * NU + 2 * DT, P0 = DIRECT ? 8 : 4, P = P0 < N ? P0 : N;
+        u32x4 f[P], w[2];
+        auto read = [&](int n) {
+          if (n < 2 * NU)
+            return *(const u32x4 *)(smem + (((n < NU ? kt : vt) + rowlane) ^ (n % NU << 5)) + base * T::PITCH);
+          return col_read<Tag, DP>(smem, kt + collane, base + (n - 2 * NU) / DT * 16, (n - 2 * NU) % DT);
+        };
+        // ds of eight states, rounded to the inputs' type for the product
+        const uint32_t bits = seen >> (4 * h);
+        auto weights = [&](int t, u32x4 *to) {
+          float ds[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) ds[i] = s[8 * t + i] * dp[8 * t + i];
+          if (seen != 0xffffffffu) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+              if (!((bits >> (16 * t + 8 * (i / 4) + i % 4)) & 1)) ds[i] = 0.f;
+          }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) (*to)[j] = pack2<Tag>(ds[2 * j], ds[2 * j + 1]);
+        };
+#pragma unroll
+        for (int n = 0; n < P; ++n) f[n] = read(n);
+        pin_order();
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+          if (n == 2 * NU) weights(0, &w[0]);
+          if (n == 2 * NU + DT) weights(1, &w[1]);
+          if (n < NU)
+            s = mma_chunk<Tag>(f[n % P], qf[n], s);
+          else if (n < 2 * NU)
+            dp = mma_chunk<Tag>(f[n % P], gf[n - NU], dp);
+          else
+            acc[(n - 2 * NU) % DT] = mma_chunk<Tag>(f[n % P], w[(n - 2 * NU) / DT], acc[(n - 2 * NU) % DT]);
+          if (n + P < N) f[n % P] = read(n + P);
+          if (n >= NU && n < 2 * NU) {
+#pragma unroll
+            for (int i = (n - NU) * 16 / NU; i < (n - NU + 1) * 16 / NU; ++i) s[i] = exp2_(s[i] * a.c);
+          }
+          pin_order();
+        }
+      } else {
+        s = rows_product<Tag, DP>(smem, kt + rowlane, base, qf, s);
+        dp = rows_product<Tag, DP>(smem, vt + rowlane, base, gf, dp);
+        to_ds(&s, dp, a.c, seen, h);
+        cols_product<Tag, DP>(smem, kt + collane, base, to_weights<Tag>(s), acc);
+      }
     }
   }
   __syncthreads();
@@ -1001,7 +1143,7 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_few_dq_kernel(Attn
 #pragma unroll
       for (int u = 0; u < T::NU; ++u) kf[u] = (u32x4){0, 0, 0, 0};
     }
-    f32x16 s = {}, dp = {};
+    f32x16 s = splat(st.x), dp = splat(st.y);
 #pragma unroll
     for (int u = 0; u < T::NU; ++u) {
       s = mma_chunk<Tag>(kf[u], qf[u], s);
@@ -1015,7 +1157,7 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_few_dq_kernel(Attn
       sight = load_sight(mask, a.mask_s, (t + 4) * 32, 32, len, lane);
     }
     // (what a hidden state's values make of dp is replaced by zero)
-    to_ds(&s, dp, a.c, st, see, h);
+    to_ds(&s, dp, a.c, see, h);
     wave_lds_fence();
     const Weights<Tag> w = to_weights<Tag>(s);
     cols_product<Tag, DP>(smem, kt + collane, 0, w, acc);
@@ -1153,13 +1295,15 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
   RowWalk<Tag, DP, VEC, F::BR> walk;
   const char *qb = a.q.p + b * a.q.b + (int64_t)hk * a.G * a.q.h, *gb = a.dout.p + b * a.dout.b + (int64_t)hk * a.G * a.dout.h;
   walk.start(a, t0 * F::BR, tid);
-  float2 st = make_float2(INFINITY, 0.f);
+  float2 st = make_float2(-INFINITY, 0.f);
   auto load = [&](int t) {
     walk.template load<DIRECT>(a, qb, gb, tid, &mq, &mg, lds_offset(smem) + (t & 1) * 2 * F::TILE, wave);
-    if (tid < F::BR) st = t * F::BR + tid < a.R ? a.rowstat[bh * a.R + t * F::BR + tid] : make_float2(INFINITY, 0.f);
+    if (tid < F::BR) st = t * F::BR + tid < a.R ? a.rowstat[bh * a.R + t * F::BR + tid] : make_float2(-INFINITY, 0.f);
   };
   f32x16 dk[DT] = {}, dv[DT] = {};
   if (t0 < t1) load(t0);
+  arrived(kf);
+  if constexpr (!F::VLDS) arrived(vf);
   for (int t = t0; t < t1; ++t) {
     const int qt = (t & 1) * 2 * F::TILE, gt = qt + F::TILE;
     float *stat = (float *)(smem + F::STAT) + (t & 1) * 2 * F::BR;
@@ -1177,31 +1321,71 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
     }
     __syncthreads();
     if (t + 1 < t1) load(t + 1);
-    f32x16 s = rows_product<Tag, DP>(smem, qt + rowlane, 0, kf);
-    f32x16 dp = {};
-    if constexpr (F::VLDS) {
-#pragma unroll
-      for (int u = 0; u < T::NU; ++u)
-        dp = mma_chunk<Tag>(*(const u32x4 *)(smem + ((gt + rowlane) ^ (u << 5))), *(const u32x4 *)(smem + (val ^ (u << 5))),
-                            dp);
-    } else {
-      dp = rows_product<Tag, DP>(smem, gt + rowlane, 0, vf);
-    }
+    // the products start from the rows' statistics
+    f32x16 s, dp;
 #pragma unroll
     for (int i = 0; i < 16; i += 4) {
-      const f32x4 l4 = *(const f32x4 *)(stat + 2 * i + 4 * h);
-      const f32x4 d4 = *(const f32x4 *)(stat + F::BR + 2 * i + 4 * h);
+      const f32x4 x = *(const f32x4 *)(stat + 2 * i + 4 * h), y = *(const f32x4 *)(stat + F::BR + 2 * i + 4 * h);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s[i + e] = exp2_(__builtin_fmaf(s[i + e], a.c, -l4[e]));
-        dp[i + e] = s[i + e] * (dp[i + e] - d4[e]);
-      }
+      for (int e = 0; e < 4; ++e) s[i + e] = x[e], dp[i + e] = y[e];
     }
-    // p and ds are rounded to the inputs' type for their products
-    const Weights<Tag> wp = to_weights<Tag>(s);
-    cols_product<Tag, DP>(smem, gt + collane, 0, wp, dv);
-    const Weights<Tag> wd = to_weights<Tag>(dp);
-    cols_product<Tag, DP>(smem, qt + collane, 0, wd, dk);
+    if constexpr (Tag::W16 && DIRECT && F::VLDS) {
+      // One stream of fragment reads, some products ahead of their use: queries
+      // for the scores, do (and the values, where they are in LDS) for dp, while
+      // which the weights are formed, then the columns of do and of the queries.
+      constexpr int NU = T::NU, N = 2 * NU + 4 * DT, P = 4, PV = 2;
+      u32x4 f[P], v[PV], w[2];
+      auto read = [&](int n) {
+        if (n < 2 * NU) return *(const u32x4 *)(smem + (((n < NU ? qt : gt) + rowlane) ^ (n % NU << 5)));
+        const int m = n - 2 * NU;
+        return col_read<Tag, DP>(smem, (m < 2 * DT ? gt : qt) + collane, m / DT % 2 * 16, m % DT);
+      };
+      // p and ds are rounded to the inputs' type for their products
+      auto pack8 = [&](const f32x16 &x, int t, u32x4 *to) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) (*to)[j] = pack2<Tag>(x[8 * t + 2 * j], x[8 * t + 2 * j + 1]);
+      };
+      auto to_ds8 = [&](int t) {
+#pragma unroll
+        for (int i = 8 * t; i < 8 * t + 8; ++i) dp[i] *= s[i];
+      };
+#pragma unroll
+      for (int n = 0; n < P; ++n) f[n] = read(n);
+      pin_order();
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        const int m = n - 2 * NU;
+        if (m == 0) pack8(s, 0, &w[0]);
+        if (m == DT) pack8(s, 1, &w[1]), to_ds8(0);
+        if (m == 2 * DT) pack8(dp, 0, &w[0]), to_ds8(1);
+        if (m == 3 * DT) pack8(dp, 1, &w[1]);
+        if (n < NU)
+          s = mma_chunk<Tag>(f[n % P], kf[n], s);
+        else if (n < 2 * NU)
+          dp = mma_chunk<Tag>(f[n % P], F::VLDS ? v[n % PV] : vf[F::VLDS ? 0 : n - NU], dp);
+        else if (m < 2 * DT)
+          dv[m % DT] = mma_chunk<Tag>(f[n % P], w[m / DT], dv[m % DT]);
+        else
+          dk[m % DT] = mma_chunk<Tag>(f[n % P], w[m / DT - 2], dk[m % DT]);
+        if (n + P < N) f[n % P] = read(n + P);
+        if (F::VLDS && n + PV >= NU && n + PV < 2 * NU) v[n % PV] = *(const u32x4 *)(smem + (val ^ ((n + PV) % NU << 5)));
+        if (n >= NU && n < 2 * NU) {
+#pragma unroll
+          for (int i = (n - NU) * 16 / NU; i < (n - NU + 1) * 16 / NU; ++i) s[i] = exp2_(s[i] * a.c);
+        }
+        pin_order();
+      }
+    } else {
+      s = rows_product<Tag, DP>(smem, qt + rowlane, 0, kf, s);
+      dp = rows_product<Tag, DP>(smem, gt + rowlane, 0, vf, dp);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[i] = exp2_(s[i] * a.c);
+        dp[i] *= s[i];
+      }
+      cols_product<Tag, DP>(smem, gt + collane, 0, to_weights<Tag>(s), dv);
+      cols_product<Tag, DP>(smem, qt + collane, 0, to_weights<Tag>(dp), dk);
+    }
   }
   if (!see) {
     // a state that is not visible has its column of results to itself
