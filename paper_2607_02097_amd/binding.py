@@ -637,7 +637,7 @@ def _empty(like, shape, dtype, stream):
 def _out_like(t, shape, out, name, stream):
     """The output tensor of t's shape (new unless given) and its tokens."""
     if out is None:
-        out = _empty(t, shape, t.dtype, stream)
+        out = torch.empty_like(t) if stream is None and t.is_contiguous() else _empty(t, shape, t.dtype, stream)
         B, S, H, D = shape
         return out, (out.data_ptr(), S * H * D, H * D, D)
     tokens = _tokens(out, name)

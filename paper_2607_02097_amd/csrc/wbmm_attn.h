@@ -507,6 +507,9 @@ __device__ inline char *group_row(const AttnArgs &a, const Tokens &t, int64_t b,
 // through `scale` what the earlier results have to be multiplied by where any
 // lane's maximum moved.
 constexpr float kLag = 8.f;
+// float16 weights are kept 2^6 larger, up to 2^14, away from the type's
+// smallest numbers.
+template <class Tag> constexpr float kRaise = __is_same(Tag, TagF16) ? 6.f : 0.f;
 
 template <int NB>
 __device__ inline bool running_top(const f32x16 *s, float c, float *top, float *fix) {
@@ -619,7 +622,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
 #pragma unroll
       for (int d = 0; d < DT; ++d) acc[d] *= fix;
     }
-    const float sub = top == -INFINITY ? 0.f : top;
+    const float sub = top == -INFINITY ? 0.f : top - kRaise<Tag>;
     if constexpr (Tag::W16) {
       // Eight weights at a time: those of the next step are formed while the
       // matrix cores take this step's.  They are rounded to the inputs' type for
@@ -693,7 +696,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   const float inv = sum == 0.f ? 0.f : 1.f / sum;
   if (a.lse && h == 0 && wk == 0 && r < a.R) {
     const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
-    a.lse[(b * a.Hq + hq) * a.Sq + sq] = sum == 0.f ? -INFINITY : (top + __builtin_amdgcn_logf(sum)) * kLn2;
+    a.lse[(b * a.Hq + hq) * a.Sq + sq] = sum == 0.f ? -INFINITY : (top - kRaise<Tag> + __builtin_amdgcn_logf(sum)) * kLn2;
   }
   __syncthreads();
   if (wk > 0) return;
@@ -792,7 +795,7 @@ __global__ __launch_bounds__(256, Tag::W16 || DP <= 64 ? 2 : 1) void attn_few_ke
 #pragma unroll
       for (int d = 0; d < DT; ++d) acc[d] *= fix;
     }
-    const float sub = top == -INFINITY ? 0.f : top;
+    const float sub = top == -INFINITY ? 0.f : top - kRaise<Tag>;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       s[i] = exp2_(__builtin_fmaf(s[i], a.c, -sub));
@@ -836,7 +839,7 @@ __global__ __launch_bounds__(256, Tag::W16 || DP <= 64 ? 2 : 1) void attn_few_ke
     }
     // a row that sees nothing: zeros, and minus infinity
     const float inv = s4 == 0.f ? 0.f : 1.f / s4;
-    const float lse2 = s4 == 0.f ? -INFINITY : t4 + __builtin_amdgcn_logf(s4);
+    const float lse2 = s4 == 0.f ? -INFINITY : t4 - kRaise<Tag> + __builtin_amdgcn_logf(s4);
     const int r = rt * 32 + n;
     if (a.splits > 1) {
       const int64_t at = (split * a.B * a.Hk + bh) * a.R + r;
@@ -900,9 +903,15 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 // dq, states for dk and dv), so every sum has one owner and a fixed order: no
 // atomics, and the same bits every time.
 
-// What the products of the lane's row start from: {-lse / scale, -delta}, so
-// that they come out as the weight's exponent and as dp - delta; a row that
-// sees nothing starts from minus infinity, and its weights come out as zero.
+// Statistics of the lane's row.  16-bit: what its products start from,
+// {-lse / scale, -delta}, so that they come out as the weight's exponent and as
+// dp - delta, without an instruction more; a row that sees nothing starts from
+// minus infinity, and its weights come out as zero.  In float32 the sums would
+// round at lse's size instead of the products' own (errors of the gradients
+// 1.3e-6 instead of 0.8e-6), so there it is {lse in log2 units, delta}, taken
+// off afterwards.
+template <class Tag> constexpr bool kStart = Tag::W16;
+constexpr float kBlind = -INFINITY;  // start of a row that sees nothing; float32: its negative
 // Kept for the kernel of dk and dv by one lane a row (`keep`).
 template <class Tag, int DP, bool VEC>
 __device__ inline float2 row_stat(const AttnArgs &a, int64_t b, int hk, int r, int lane, const u32x4 *gf, bool keep) {
@@ -922,11 +931,11 @@ __device__ inline float2 row_stat(const AttnArgs &a, int64_t b, int hk, int r, i
         d += __uint_as_float(x) * __uint_as_float(y);
     }
   d = other_half_sum(d);
-  float2 st = make_float2(-INFINITY, 0.f);
+  float2 st = make_float2(kStart<Tag> ? kBlind : -kBlind, 0.f);
   if (r < a.R) {
     const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
     const float lse = a.lse[(b * a.Hq + hq) * a.Sq + sq];
-    if (lse != -INFINITY) st = make_float2(-lse / a.scale, -d);
+    if (lse != -INFINITY) st = kStart<Tag> ? make_float2(-lse / a.scale, -d) : make_float2(lse * kLog2e, d);
     if (keep && lane < 32) a.rowstat[(b * a.Hk + hk) * a.R + r] = st;
   }
   return st;
@@ -942,11 +951,18 @@ __device__ inline f32x16 splat(float v) {
   return r;
 }
 
-// Exponents and dp - delta to ds (one lane: 16 states of one row), zero where
-// not visible.
-__device__ inline void to_ds(f32x16 *s, const f32x16 &dp, float c, uint32_t seen, int h) {
+// Weight of one state and ds, from what the products gave.
+template <class Tag> __device__ inline float weight(float s, float c, float x) {
+  return kStart<Tag> ? exp2_(s * c) : exp2_(__builtin_fmaf(s, c, -x));
+}
+template <class Tag> __device__ inline float ds_of(float p, float dp, float y) { return kStart<Tag> ? p * dp : p * (dp - y); }
+
+// The products' results to ds (one lane: 16 states of one row), zero where not
+// visible.
+template <class Tag>
+__device__ inline void to_ds(f32x16 *s, const f32x16 &dp, float c, float2 st, uint32_t seen, int h) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) (*s)[i] = exp2_((*s)[i] * c) * dp[i];
+  for (int i = 0; i < 16; ++i) (*s)[i] = ds_of<Tag>(weight<Tag>((*s)[i], c, st.x), dp[i], st.y);
   if (seen != 0xffffffffu) {
     const uint32_t bits = seen >> (4 * h);
 #pragma unroll
@@ -1013,7 +1029,7 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
       const int base = wk * F::KW + 32 * k;
-      f32x16 s = splat(st.x), dp = splat(st.y);
+      f32x16 s = splat(kStart<Tag> ? st.x : 0.f), dp = splat(kStart<Tag> ? st.y : 0.f);
       const uint32_t seen = (uint32_t)(see >> base);
       if constexpr (Tag::W16 && DIRECT) {
         // One stream of fragment reads, some products ahead of their use: keys
@@ -1063,7 +1079,7 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs
       } else {
         s = rows_product<Tag, DP>(smem, kt + rowlane, base, qf, s);
         dp = rows_product<Tag, DP>(smem, vt + rowlane, base, gf, dp);
-        to_ds(&s, dp, a.c, seen, h);
+        to_ds<Tag>(&s, dp, a.c, st, seen, h);
         cols_product<Tag, DP>(smem, kt + collane, base, to_weights<Tag>(s), acc);
       }
     }
@@ -1143,7 +1159,7 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_few_dq_kernel(Attn
 #pragma unroll
       for (int u = 0; u < T::NU; ++u) kf[u] = (u32x4){0, 0, 0, 0};
     }
-    f32x16 s = splat(st.x), dp = splat(st.y);
+    f32x16 s = splat(kStart<Tag> ? st.x : 0.f), dp = splat(kStart<Tag> ? st.y : 0.f);
 #pragma unroll
     for (int u = 0; u < T::NU; ++u) {
       s = mma_chunk<Tag>(kf[u], qf[u], s);
@@ -1157,7 +1173,7 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_few_dq_kernel(Attn
       sight = load_sight(mask, a.mask_s, (t + 4) * 32, 32, len, lane);
     }
     // (what a hidden state's values make of dp is replaced by zero)
-    to_ds(&s, dp, a.c, see, h);
+    to_ds<Tag>(&s, dp, a.c, st, see, h);
     wave_lds_fence();
     const Weights<Tag> w = to_weights<Tag>(s);
     cols_product<Tag, DP>(smem, kt + collane, 0, w, acc);
@@ -1295,10 +1311,14 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
   RowWalk<Tag, DP, VEC, F::BR> walk;
   const char *qb = a.q.p + b * a.q.b + (int64_t)hk * a.G * a.q.h, *gb = a.dout.p + b * a.dout.b + (int64_t)hk * a.G * a.dout.h;
   walk.start(a, t0 * F::BR, tid);
-  float2 st = make_float2(-INFINITY, 0.f);
+  const float2 blind = make_float2(kStart<Tag> ? kBlind : -kBlind, 0.f);
+  float2 st = blind;
   auto load = [&](int t) {
     walk.template load<DIRECT>(a, qb, gb, tid, &mq, &mg, lds_offset(smem) + (t & 1) * 2 * F::TILE, wave);
-    if (tid < F::BR) st = t * F::BR + tid < a.R ? a.rowstat[bh * a.R + t * F::BR + tid] : make_float2(-INFINITY, 0.f);
+    if (tid < F::BR) {
+      st = blind;
+      if (t * F::BR + tid < a.R) st = a.rowstat[bh * a.R + t * F::BR + tid];
+    }
   };
   f32x16 dk[DT] = {}, dv[DT] = {};
   if (t0 < t1) load(t0);
@@ -1321,13 +1341,14 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
     }
     __syncthreads();
     if (t + 1 < t1) load(t + 1);
-    // the products start from the rows' statistics
-    f32x16 s, dp;
+    f32x16 s = {}, dp = {};
+    if constexpr (kStart<Tag>) {
 #pragma unroll
-    for (int i = 0; i < 16; i += 4) {
-      const f32x4 x = *(const f32x4 *)(stat + 2 * i + 4 * h), y = *(const f32x4 *)(stat + F::BR + 2 * i + 4 * h);
+      for (int i = 0; i < 16; i += 4) {
+        const f32x4 x = *(const f32x4 *)(stat + 2 * i + 4 * h), y = *(const f32x4 *)(stat + F::BR + 2 * i + 4 * h);
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[i + e] = x[e], dp[i + e] = y[e];
+        for (int e = 0; e < 4; ++e) s[i + e] = x[e], dp[i + e] = y[e];
+      }
     }
     if constexpr (Tag::W16 && DIRECT && F::VLDS) {
       // One stream of fragment reads, some products ahead of their use: queries
@@ -1379,9 +1400,17 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
       s = rows_product<Tag, DP>(smem, qt + rowlane, 0, kf, s);
       dp = rows_product<Tag, DP>(smem, gt + rowlane, 0, vf, dp);
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        s[i] = exp2_(s[i] * a.c);
-        dp[i] *= s[i];
+      for (int i = 0; i < 16; i += 4) {
+        f32x4 x = {}, y = {};
+        if constexpr (!kStart<Tag>) {
+          x = *(const f32x4 *)(stat + 2 * i + 4 * h);
+          y = *(const f32x4 *)(stat + F::BR + 2 * i + 4 * h);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[i + e] = weight<Tag>(s[i + e], a.c, x[e]);
+          dp[i + e] = ds_of<Tag>(s[i + e], dp[i + e], y[e]);
+        }
       }
       cols_product<Tag, DP>(smem, gt + collane, 0, to_weights<Tag>(s), dv);
       cols_product<Tag, DP>(smem, qt + collane, 0, to_weights<Tag>(dp), dk);

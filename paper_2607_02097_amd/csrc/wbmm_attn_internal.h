@@ -54,7 +54,7 @@ struct AttnArgs {
   // and, forward, part_l [splits, B Hk, R] (lse in log2 units).
   int tile_rows, splits;
   float *part_o, *part_l;
-  // backward: per row {lse in log2 units, delta}, [B Hk, R]
+  // backward: two statistics per row, [B Hk, R] (row_stat)
   float2 *rowstat;
   // backward: dk, dv in `row_parts` parts of the rows, with partial sums
   // part_dk, part_dv [row_parts, B Hk, Sk, D]

@@ -53,12 +53,6 @@ template <class Tag> __device__ inline u32x4 repack(const float *f) {
   return v;
 }
 
-template <class Tag> __device__ inline float load1(const char *p) {
-  if constexpr (Tag::W16)
-    return to_f32<Tag>(*(const u16 *)p);
-  else
-    return *(const float *)p;
-}
 template <class Tag> __device__ inline void store1(char *p, float v) {
   if constexpr (Tag::W16)
     *(u16 *)p = (u16)pack2<Tag>(v, 0.f);
@@ -73,6 +67,7 @@ struct RotPlan {
   int tok;        // tokens of a workgroup
   int heads;      // heads of a workgroup (grid dimension y counts the runs)
   int turn, per;  // turning items of a head, all items of a head
+  int small;      // tokens are counted in 32 bits
   uint32_t magic, magic_tok;  // ceil(2^32 / per), ceil(2^32 / items of a token); 0 for 1
 };
 
@@ -80,24 +75,90 @@ struct RotPlan {
 __device__ inline int quotient(int e, uint32_t magic) { return magic ? (int)__umulhi((uint32_t)e, magic) : e; }
 inline uint32_t reciprocal(int64_t d) { return d == 1 ? 0 : (uint32_t)((((uint64_t)1 << 32) + d - 1) / d); }
 
-template <class Tag, bool VEC>
+// (Written out as fused products, so that every layout gives the same bits.)
+__device__ inline void rotate(float *lo, float *hi, float2 r) {
+  const float u = *lo, w = *hi;
+  *lo = __builtin_fmaf(-w, r.y, u * r.x);
+  *hi = __builtin_fmaf(u, r.y, w * r.x);
+}
+
+// Results are not read again here; kept out of the caches' way they leave
+// faster: 12544 x 40 x 128 bfloat16 44.8 -> 40.0 us, 16000 x 24 x 128 float32
+// 77 -> 60 us (6.6 TB/s).
+__device__ inline void store16(char *p, u32x4 v) { __builtin_nontemporal_store(v, (u32x4 *)p); }
+
+// Where an item's components lie in its row: up to two pieces of a head.
+struct RotItem {
+  int t, pos;        // token of the workgroup; first pair, or -1: copied
+  int64_t x, y;      // bytes from the token's first component
+  int64_t next;      // the second piece of a pair, behind the first (half layout)
+};
+
+template <class Tag, bool VEC, bool ADJ>
 __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a, RotPlan pl) {
-  constexpr int V = 16 / Tag::ES;
-  extern __shared__ __align__(16) float2 cs[];  // [tok][P]
+  constexpr int V = VEC ? 16 / Tag::ES : 1;  // components of a piece
+  constexpr int U = 2;                       // items whose loads leave together
+  extern __shared__ __align__(16) float2 cs[];  // [tok][P], then the tokens' x and y
+  int64_t *const at = (int64_t *)(cs + pl.tok * a.P);
   const int tid = threadIdx.x;
   const int64_t n0 = (int64_t)blockIdx.x * pl.tok;
   const int64_t left = a.B * a.S - n0;
   const int ntok = left < pl.tok ? (int)left : pl.tok;
   const int h0 = blockIdx.y * pl.heads;
   const int nh = a.H - h0 < pl.heads ? a.H - h0 : pl.heads;
+  if (tid < ntok) {
+    const int64_t n = n0 + tid, b = pl.small ? (int64_t)((uint32_t)n / (uint32_t)a.S) : n / a.S, s = n - b * a.S;
+    at[2 * tid] = b * a.x.b + s * a.x.s;
+    at[2 * tid + 1] = b * a.y.b + s * a.y.s;
+  }
+  __syncthreads();
+  const int per_token = nh * pl.per, items = ntok * per_token;
+  auto item = [&](int g) {
+    // (several tokens only with all heads in one run, so that per_token is the plan's)
+    RotItem r;
+    r.t = pl.tok == 1 ? 0 : quotient(g, pl.magic_tok);
+    const int e = g - r.t * per_token;
+    const int hd = quotient(e, pl.magic), i = e - hd * pl.per;
+    const bool turn = i < pl.turn;
+    const int piece = turn ? (ADJ && !VEC ? 2 * i : i * V) : 2 * a.P + (i - pl.turn) * V;
+    r.pos = turn ? (ADJ && VEC ? i * V / 2 : i * V) : -1;
+    r.x = at[2 * r.t] + (int64_t)(h0 + hd) * a.x.h + piece * Tag::ES;
+    r.y = at[2 * r.t + 1] + (int64_t)(h0 + hd) * a.y.h + piece * Tag::ES;
+    r.next = (ADJ ? (VEC ? 0 : 1) : a.P) * Tag::ES;
+    return r;
+  };
+  // the first items' loads are under way while the angles are computed
+  u32x4 lo[U], hi[U];
+  RotItem it[U];
+  auto load = [&](int g0) {
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int g = g0 + j * kRotThreads;
+      it[j].t = -1;
+      if (g >= items) continue;
+      it[j] = item(g);
+      const char *p = a.x.p + it[j].x;
+      if constexpr (VEC) {
+        lo[j] = *(const u32x4 *)p;
+        if (!ADJ && it[j].pos >= 0) hi[j] = *(const u32x4 *)(p + it[j].next);
+      } else if constexpr (Tag::W16) {
+        lo[j][0] = *(const u16 *)p;
+        if (it[j].pos >= 0) hi[j][0] = *(const u16 *)(p + it[j].next);
+      } else {
+        lo[j][0] = *(const uint32_t *)p;
+        if (it[j].pos >= 0) hi[j][0] = *(const uint32_t *)(p + it[j].next);
+      }
+    }
+  };
+  load(tid);
   for (int e = tid; e < ntok * a.P; e += kRotThreads) {
     const int t = e / a.P, i = e - t * a.P;
-    const int64_t n = n0 + t, b = n / a.S, s = n - b * a.S;
+    const int64_t n = n0 + t, b = pl.small ? (int64_t)((uint32_t)n / (uint32_t)a.S) : n / a.S, s = n - b * a.S;
     int axis = 0;
 #pragma unroll
     for (int j = 0; j + 1 < kMaxAxes; ++j) axis += j + 1 < a.axes && i >= a.first[j];
-    const int64_t at = axis * a.pos_a + b * a.pos_b + s * a.pos_s;
-    const double p = a.pos64 ? (double)((const int64_t *)a.pos)[at] : (double)((const int32_t *)a.pos)[at];
+    const int64_t pa = axis * a.pos_a + b * a.pos_b + s * a.pos_s;
+    const double p = a.pos64 ? (double)((const int64_t *)a.pos)[pa] : (double)((const int32_t *)a.pos)[pa];
     const double turns = p * (double)a.freqs[i] * 0.15915494309189533577;
     const float half = (float)(2.0 * (turns - rint(turns)));  // half turns, -1 .. 1
     float sn, cn;
@@ -105,63 +166,54 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a, RotPl
     cs[e] = make_float2(cn, a.reverse ? -sn : sn);
   }
   __syncthreads();
-  const int per_token = nh * pl.per, items = ntok * per_token;
-  for (int g = tid; g < items; g += kRotThreads) {
-    // (several tokens only with all heads in one run, so that per_token is the plan's)
-    const int t = pl.tok == 1 ? 0 : quotient(g, pl.magic_tok);
-    const int e = g - t * per_token;
-    const int hd = quotient(e, pl.magic), i = e - hd * pl.per;
-    const int64_t n = n0 + t, b = n / a.S, s = n - b * a.S;
-    const float2 *ct = cs + t * a.P;
-    {
-      const char *xr = a.x.p + b * a.x.b + s * a.x.s;
-      char *yr = a.y.p + b * a.y.b + s * a.y.s;
-      const char *xh = xr + (int64_t)(h0 + hd) * a.x.h;
-      char *yh = yr + (int64_t)(h0 + hd) * a.y.h;
+  for (int g0 = tid; g0 < items; g0 += U * kRotThreads) {
+    if (g0 != tid) load(g0);
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      if (it[j].t < 0) continue;
+      char *q = a.y.p + it[j].y;
+      const float2 *ct = cs + it[j].t * a.P + it[j].pos;
       if constexpr (VEC) {
-        if (i < pl.turn && !a.adjacent) {
-          const int o = i * 16, o2 = o + a.P * Tag::ES;
-          const u32x4 lo = *(const u32x4 *)(xh + o), hi = *(const u32x4 *)(xh + o2);
-          float fl[V], fh[V];
-          unpack<Tag>(lo, fl);
-          unpack<Tag>(hi, fh);
-#pragma unroll
-          for (int j = 0; j < V; ++j) {
-            const float2 r = ct[i * V + j];
-            const float u = fl[j], w = fh[j];
-            fl[j] = u * r.x - w * r.y;
-            fh[j] = u * r.y + w * r.x;
-          }
-          *(u32x4 *)(yh + o) = repack<Tag>(fl);
-          *(u32x4 *)(yh + o2) = repack<Tag>(fh);
-        } else if (i < pl.turn) {
+        if (it[j].pos < 0) {
+          store16(q, lo[j]);
+        } else if constexpr (ADJ) {
           float f[V];
-          unpack<Tag>(*(const u32x4 *)(xh + i * 16), f);
+          unpack<Tag>(lo[j], f);
 #pragma unroll
-          for (int j = 0; j < V; j += 2) {
-            const float2 r = ct[(i * V + j) / 2];
-            const float u = f[j], w = f[j + 1];
-            f[j] = u * r.x - w * r.y;
-            f[j + 1] = u * r.y + w * r.x;
+          for (int k = 0; k < V; k += 2) {
+            const float2 r = ct[k / 2];
+            rotate(&f[k], &f[k + 1], r);
           }
-          *(u32x4 *)(yh + i * 16) = repack<Tag>(f);
+          store16(q, repack<Tag>(f));
         } else {
-          const int o = 2 * a.P * Tag::ES + (i - pl.turn) * 16;
-          *(u32x4 *)(yh + o) = *(const u32x4 *)(xh + o);
+          float fl[V], fh[V];
+          unpack<Tag>(lo[j], fl);
+          unpack<Tag>(hi[j], fh);
+#pragma unroll
+          for (int k = 0; k < V; ++k) {
+            const float2 r = ct[k];
+            rotate(&fl[k], &fh[k], r);
+          }
+          store16(q, repack<Tag>(fl));
+          store16(q + it[j].next, repack<Tag>(fh));
         }
       } else {
-        if (i < pl.turn) {
-          const int o = (a.adjacent ? 2 * i : i) * Tag::ES, o2 = o + (a.adjacent ? 1 : a.P) * Tag::ES;
-          const float2 r = ct[i];
-          const float u = load1<Tag>(xh + o), w = load1<Tag>(xh + o2);
-          store1<Tag>(yh + o, u * r.x - w * r.y);
-          store1<Tag>(yh + o2, u * r.y + w * r.x);
-        } else {
-          const int o = (2 * a.P + i - pl.turn) * Tag::ES;
+        const uint32_t l = lo[j][0], m = hi[j][0];
+        if (it[j].pos < 0) {
           if constexpr (Tag::W16)
-            *(u16 *)(yh + o) = *(const u16 *)(xh + o);
+            *(u16 *)q = (u16)l;
           else
-            *(float *)(yh + o) = *(const float *)(xh + o);
+            *(uint32_t *)q = l;
+        } else {
+          float u, w;
+          if constexpr (Tag::W16)
+            u = to_f32<Tag>((u16)l), w = to_f32<Tag>((u16)m);
+          else
+            u = __uint_as_float(l), w = __uint_as_float(m);
+          const float2 r = *ct;
+          rotate(&u, &w, r);
+          store1<Tag>(q, u);
+          store1<Tag>(q + it[j].next, w);
         }
       }
     }
@@ -189,11 +241,19 @@ hipError_t launch(const RotaryArgs &a, hipStream_t stream) {
   const int64_t blocks = (n + pl.tok - 1) / pl.tok;
   if (blocks > (1 << 23) || runs > 65535) return hipErrorInvalidConfiguration;
   const dim3 grid((unsigned)blocks, (unsigned)runs);
-  const size_t lds = (size_t)pl.tok * a.P * sizeof(float2);
-  if (vec)
-    rotary_kernel<Tag, true><<<grid, kRotThreads, lds, stream>>>(a, pl);
-  else
-    rotary_kernel<Tag, false><<<grid, kRotThreads, lds, stream>>>(a, pl);
+  pl.small = n < ((int64_t)1 << 31);
+  const size_t lds = (size_t)pl.tok * (a.P * sizeof(float2) + 16);
+  if (vec) {
+    if (a.adjacent)
+      rotary_kernel<Tag, true, true><<<grid, kRotThreads, lds, stream>>>(a, pl);
+    else
+      rotary_kernel<Tag, true, false><<<grid, kRotThreads, lds, stream>>>(a, pl);
+  } else {
+    if (a.adjacent)
+      rotary_kernel<Tag, false, true><<<grid, kRotThreads, lds, stream>>>(a, pl);
+    else
+      rotary_kernel<Tag, false, false><<<grid, kRotThreads, lds, stream>>>(a, pl);
+  }
   return hipGetLastError();
 }
 
