@@ -305,14 +305,18 @@ __device__ inline void store_rows(char *piece, const f32x16 *acc, float f, int D
         *(f32x4 *)at = (f32x4){a, b, c, d};
     }
   wave_lds_fence();
-  constexpr int RPP = 64 / T::LPC;
+  constexpr int RPP = 64 / T::LPC, NP = 32 / RPP;
   const int c = lane % T::LPC;
+  u32x4 v[NP];
 #pragma unroll
-  for (int p = 0; p < 32 / RPP; ++p) {
+  for (int p = 0; p < NP; ++p) {
     const int rw = p * RPP + lane / T::LPC;
-    char *row = row_at(rw);
-    if (row)
-      store_chunk<Tag, VEC>(row, c * T::CE, D, *(const u32x4 *)(piece + rw * T::PITCH + ((c ^ T::swz(rw)) << 4)));
+    v[p] = *(const u32x4 *)(piece + rw * T::PITCH + ((c ^ T::swz(rw)) << 4));
+  }
+#pragma unroll
+  for (int p = 0; p < NP; ++p) {
+    char *row = row_at(p * RPP + lane / T::LPC);
+    if (row) store_chunk<Tag, VEC>(row, c * T::CE, D, v[p]);
   }
   wave_lds_fence();
 }
@@ -1436,6 +1440,183 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
   store_rows<Tag, DP, VEC>(smem + wave * F::OUT, dv, 1.f, a.D, lane, [&](int n) { return row(a.dv, n); });
 }
 
+// All gradients of a handful of rows in one pass over the states (16-bit, at
+// most 64 components and 64 rows a key head: learned queries that read a map):
+// the states, read and written once, bound it.  A workgroup keeps a key head's
+// rows in LDS and takes a part of its states; each wave runs over every fourth
+// block of 32, on its own.  The scores are taken as for dk and dv; for dq the
+// block's ds goes through LDS to turn a lane's rows into its column.  dq is
+// summed over the waves at the end, over the parts by attn_sum_kernel.
+template <class Tag, int DP>
+struct RowsShape {
+  static constexpr int PITCH = Tile<Tag, DP>::PITCH;
+  static constexpr int ROWS = 64, NRB = 2;
+  static constexpr int Q = 0, G = ROWS * PITCH, STAT = 2 * ROWS * PITCH;
+  static constexpr int DS = 32 * Tile<Tag, 32>::PITCH;  // a wave's ds: 32 states of 32 rows
+  static constexpr int WAVE = 2 * 32 * PITCH + DS;      // a wave's keys, values and ds
+  static constexpr int W0 = STAT + 2 * ROWS * 4;
+  static constexpr int JOIN = 3 * NRB * 16 * (DP / 32) * 64 * 4;
+  static constexpr int LDS = W0 + 4 * WAVE > JOIN ? W0 + 4 * WAVE : JOIN;
+};
+
+template <class Tag, int DP, bool VEC>
+__global__ __launch_bounds__(256, 2) void attn_rows_bwd_kernel(AttnArgs a) {
+  using T = Tile<Tag, DP>;
+  using T32 = Tile<Tag, 32>;
+  using F = RowsShape<Tag, DP>;
+  constexpr int DT = T::DT, NU = T::NU;
+  extern __shared__ __align__(512) char attn_smem[];
+  char *const smem = attn_smem;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h = lane >> 5, l31 = lane & 31;
+  const int64_t unit = unit_of(blockIdx.x, gridDim.x), bh = unit / a.splits, b = bh / a.Hk;
+  const int split = (int)(unit - bh * a.splits), hk = (int)(bh - b * a.Hk);
+  const int len = length_of(a, b);
+  const int all = (a.Sk + 31) / 32;
+  const int t0 = (int)((int64_t)all * split / a.splits), t1 = (int)((int64_t)all * (split + 1) / a.splits);
+  const int nrb = a.R > 32 ? 2 : 1;
+  const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
+  const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
+  const int rowlane = T::rowlane(lane), collane = T::collane(lane), col32 = T32::collane(lane);
+  const int kt = F::W0 + wave * F::WAVE, vt = kt + 32 * F::PITCH, dst = vt + 32 * F::PITCH;
+
+  StateMover<Tag, DP, VEC, 32, 64> mk, mv;
+  uint32_t sight = 1;
+  auto load = [&](int t) {
+    if (t * 32 >= len) return;
+    mk.load(kb, a.k.s, t * 32, len, a.D, lane);
+    mv.load(vb, a.v.s, t * 32, len, a.D, lane);
+    sight = load_sight(mask, a.mask_s, t * 32, 32, len, lane);
+  };
+  int t = t0 + wave;
+  if (t < t1) load(t);
+  {
+    Mover<Tag, DP, F::ROWS, 256> mq, mg;
+    RowWalk<Tag, DP, VEC, F::ROWS> walk;
+    walk.start(a, 0, tid);
+    walk.template load<false>(a, a.q.p + b * a.q.b + (int64_t)hk * a.G * a.q.h,
+                              a.dout.p + b * a.dout.b + (int64_t)hk * a.G * a.dout.h, tid, &mq, &mg, 0, 0);
+    mq.cut(a.D, tid);
+    mg.cut(a.D, tid);
+    mq.store(smem + F::Q, tid);
+    mg.store(smem + F::G, tid);
+    if (wave < F::NRB) {
+      u32x4 gf[NU];
+      const int r = wave * 32 + l31;
+      load_rows<Tag, DP, VEC>(a, a.dout, b, hk, r, lane, gf);
+      const float2 st = row_stat<Tag, DP, VEC>(a, b, hk, r, lane, gf, false);
+      if (h == 0) {
+        ((float *)(smem + F::STAT))[r] = st.x;
+        ((float *)(smem + F::STAT))[F::ROWS + r] = st.y;
+      }
+    }
+  }
+  __syncthreads();
+
+  f32x16 dq[F::NRB][DT] = {};
+  for (; t < t1; t += 4) {
+    const int j0 = t * 32;
+    f32x16 dk[DT] = {}, dv[DT] = {};
+    if (j0 < len) {
+      uint32_t see = 0xffffffffu;
+      if (mask || j0 + 32 > len) see = (uint32_t)sight_bits(sight, j0, 32, len, lane);
+      const bool hide = see != 0xffffffffu;
+      mk.hide(hide, see, a.D, lane);
+      mv.hide(hide, see, a.D, lane);
+      mk.store(smem + kt, lane);
+      mv.store(smem + vt, lane);
+      if (t + 4 < t1) load(t + 4);
+      wave_lds_fence();
+#pragma unroll
+      for (int rb = 0; rb < F::NRB; ++rb) {
+        if (rb >= nrb) continue;
+        const float *stat = (const float *)(smem + F::STAT) + rb * 32;
+        f32x16 s, dp;
+#pragma unroll
+        for (int i = 0; i < 16; i += 4) {
+          const f32x4 x = *(const f32x4 *)(stat + 2 * i + 4 * h), y = *(const f32x4 *)(stat + F::ROWS + 2 * i + 4 * h);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[i + e] = x[e], dp[i + e] = y[e];
+        }
+#pragma unroll
+        for (int u = 0; u < NU; ++u) {
+          const int x = u << 5;
+          s = mma_chunk<Tag>(*(const u32x4 *)(smem + ((F::Q + rowlane) ^ x) + rb * 32 * F::PITCH),
+                             *(const u32x4 *)(smem + ((kt + rowlane) ^ x)), s);
+          dp = mma_chunk<Tag>(*(const u32x4 *)(smem + ((F::G + rowlane) ^ x) + rb * 32 * F::PITCH),
+                              *(const u32x4 *)(smem + ((vt + rowlane) ^ x)), dp);
+        }
+        if (hide && !((see >> l31) & 1)) s = splat(-INFINITY);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          s[i] = exp2_(s[i] * a.c);
+          dp[i] *= s[i];
+        }
+        // p and ds are rounded to the inputs' type for their products
+        const Weights<Tag> wd = to_weights<Tag>(dp);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          *(u32x2 *)(smem + dst + l31 * T32::PITCH + ((i ^ T32::swz(l31)) << 4) + 8 * h) =
+              (u32x2){wd.w[i / 2][i % 2 * 2], wd.w[i / 2][i % 2 * 2 + 1]};
+        cols_product<Tag, DP>(smem, F::G + collane, rb * 32, to_weights<Tag>(s), dv);
+        cols_product<Tag, DP>(smem, F::Q + collane, rb * 32, wd, dk);
+        wave_lds_fence();
+        Weights<Tag> wq;
+#pragma unroll
+        for (int i = 0; i < 2; ++i) wq.w[i] = col_read<Tag, 32>(smem, dst + col32, 16 * i, 0);
+        cols_product<Tag, DP>(smem, kt + collane, 0, wq, dq[rb]);
+        wave_lds_fence();
+      }
+    }
+    auto row = [&](const Tokens &o, int n) {
+      return j0 + n < a.Sk ? o.p + b * o.b + (j0 + n) * o.s + hk * o.h : nullptr;
+    };
+    store_rows<Tag, DP, VEC>(smem + vt, dv, 1.f, a.D, lane, [&](int n) { return row(a.dv, n); });
+    store_rows<Tag, DP, VEC>(smem + kt, dk, a.scale, a.D, lane, [&](int n) { return row(a.dk, n); });
+  }
+
+  // the waves' parts of dq
+  __syncthreads();
+  float *xo = (float *)smem;  // [wave - 1][16 NRB DT][64]
+  constexpr int PER = 16 * F::NRB * DT * 64;
+  if (wave > 0) {
+    float *o = xo + (wave - 1) * PER + lane;
+#pragma unroll
+    for (int rb = 0; rb < F::NRB; ++rb)
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[((rb * DT + d) * 16 + i) * 64] = dq[rb][d][i];
+  }
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll
+  for (int rb = 0; rb < F::NRB; ++rb)
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        float x = dq[rb][d][i];
+#pragma unroll
+        for (int w = 0; w < 3; ++w) x += xo[w * PER + ((rb * DT + d) * 16 + i) * 64 + lane];
+        dq[rb][d][i] = x;
+      }
+#pragma unroll
+  for (int rb = 0; rb < F::NRB; ++rb) {
+    if (rb >= nrb) continue;
+    if (a.splits > 1) {
+      float *p = a.part_o + (split * a.B * a.Hk + bh) * a.R * a.D;
+      store_rows<TagF32, DP, VEC>(smem, dq[rb], a.scale, a.D, lane, [&](int n) {
+        const int r = rb * 32 + n;
+        return r < a.R ? (char *)(p + (int64_t)r * a.D) : nullptr;
+      });
+    } else {
+      store_rows<Tag, DP, VEC>(smem, dq[rb], a.scale, a.D, lane,
+                               [&](int n) { return group_row(a, a.dq, b, hk, rb * 32 + n); });
+    }
+  }
+}
+
 // Sums of partial gradients, in the order of the parts: rows [B Hk, N] of D
 // components, row n of key head hk being token n / G of head hk G + n % G.
 // Blocks of y = 1 take the second tensor.
@@ -1504,6 +1685,16 @@ hipError_t launch_fwd(const AttnArgs &a, hipStream_t stream) {
 template <class Tag, int DP, bool VEC>
 hipError_t launch_bwd(const AttnArgs &a, hipStream_t stream) {
   const int64_t bh = a.B * a.Hk;
+  if constexpr (Tag::W16 && DP <= 64) {
+    if (a.one_pass) {
+      WBMM_ATTN_LAUNCH((attn_rows_bwd_kernel<Tag, DP, VEC>), bh * a.splits, (RowsShape<Tag, DP>::LDS), a);
+      if (a.splits > 1) {
+        const SumArgs s = {{a.part_o}, {a.dq}, bh * a.R, a.splits, a.R, a.G, a.Hk, a.D};
+        WBMM_ATTN_LAUNCH((attn_sum_kernel<Tag>), (bh * a.R * a.D + 255) / 256, 0, s);
+      }
+      return hipSuccess;
+    }
+  }
   if (a.R > 0) {
     if (a.tile_rows == 32) {
       WBMM_ATTN_LAUNCH((attn_few_dq_kernel<Tag, DP, VEC>), bh * ((a.R + 31) / 32) * a.splits,

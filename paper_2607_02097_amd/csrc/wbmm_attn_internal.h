@@ -53,6 +53,7 @@ struct AttnArgs {
   // states go in `splits` parts with partial results part_o [splits, B Hk, R, D]
   // and, forward, part_l [splits, B Hk, R] (lse in log2 units).
   int tile_rows, splits;
+  int one_pass;  // backward: one kernel for all gradients, of `splits` parts
   float *part_o, *part_l;
   // backward: two statistics per row, [B Hk, R] (row_stat)
   float2 *rowstat;
