@@ -1450,7 +1450,7 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
 template <class Tag, int DP>
 struct RowsShape {
   static constexpr int PITCH = Tile<Tag, DP>::PITCH;
-  static constexpr int ROWS = 64, NRB = 2;
+  static constexpr int NRB = DP <= 64 ? 2 : 1, ROWS = 32 * NRB;
   static constexpr int Q = 0, G = ROWS * PITCH, STAT = 2 * ROWS * PITCH;
   static constexpr int DS = 32 * Tile<Tag, 32>::PITCH;  // a wave's ds: 32 states of 32 rows
   static constexpr int WAVE = 2 * 32 * PITCH + DS;      // a wave's keys, values and ds
@@ -1460,7 +1460,7 @@ struct RowsShape {
 };
 
 template <class Tag, int DP, bool VEC>
-__global__ __launch_bounds__(256, 2) void attn_rows_bwd_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(AttnArgs a) {
   using T = Tile<Tag, DP>;
   using T32 = Tile<Tag, 32>;
   using F = RowsShape<Tag, DP>;
@@ -1685,7 +1685,7 @@ hipError_t launch_fwd(const AttnArgs &a, hipStream_t stream) {
 template <class Tag, int DP, bool VEC>
 hipError_t launch_bwd(const AttnArgs &a, hipStream_t stream) {
   const int64_t bh = a.B * a.Hk;
-  if constexpr (Tag::W16 && DP <= 64) {
+  if constexpr (Tag::W16) {
     if (a.one_pass) {
       WBMM_ATTN_LAUNCH((attn_rows_bwd_kernel<Tag, DP, VEC>), bh * a.splits, (RowsShape<Tag, DP>::LDS), a);
       if (a.splits > 1) {

@@ -371,7 +371,7 @@ void attn_plan_forward(Dt, AttnArgs *a) {
 // of 256 rows and 784 states 40 us in one and 47 in two.
 void attn_plan_backward(Dt dt, AttnArgs *a) {
   plan_rows(a);
-  if (dt != Dt::F32 && a->D <= 64 && a->R > 0 && a->R <= 64 && a->Sk > 0) {
+  if (dt != Dt::F32 && a->R > 0 && a->R <= (a->D <= 64 ? 64 : 32) && a->Sk > 0) {
     a->one_pass = a->row_parts = 1;
     const int64_t bh = a->B * a->Hk;
     a->splits = (int)clamp(bh > 0 ? 2 * kUnits / bh : 1, 1, clamp(cdiv(a->Sk, 256), 1, 64));
