@@ -1441,16 +1441,16 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
 }
 
 // All gradients of a handful of rows in one pass over the states (16-bit, at
-// most 64 components and 64 rows a key head: learned queries that read a map):
-// the states, read and written once, bound it.  A workgroup keeps a key head's
+// most one_pass_rows a key head: learned queries that read a map): the states,
+// read and written once, bound it.  A workgroup keeps a key head's
 // rows in LDS and takes a part of its states; each wave runs over every fourth
 // block of 32, on its own.  The scores are taken as for dk and dv; for dq the
 // block's ds goes through LDS to turn a lane's rows into its column.  dq is
 // summed over the waves at the end, over the parts by attn_sum_kernel.
-template <class Tag, int DP>
+template <class Tag, int DP, int NRB_>
 struct RowsShape {
   static constexpr int PITCH = Tile<Tag, DP>::PITCH;
-  static constexpr int NRB = DP <= 64 ? 2 : 1, ROWS = 32 * NRB;
+  static constexpr int NRB = NRB_, ROWS = 32 * NRB;
   static constexpr int Q = 0, G = ROWS * PITCH, STAT = 2 * ROWS * PITCH;
   static constexpr int DS = 32 * Tile<Tag, 32>::PITCH;  // a wave's ds: 32 states of 32 rows
   static constexpr int WAVE = 2 * 32 * PITCH + DS;      // a wave's keys, values and ds
@@ -1459,11 +1459,11 @@ struct RowsShape {
   static constexpr int LDS = W0 + 4 * WAVE > JOIN ? W0 + 4 * WAVE : JOIN;
 };
 
-template <class Tag, int DP, bool VEC>
+template <class Tag, int DP, int NRB, bool VEC>
 __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(AttnArgs a) {
   using T = Tile<Tag, DP>;
   using T32 = Tile<Tag, 32>;
-  using F = RowsShape<Tag, DP>;
+  using F = RowsShape<Tag, DP, NRB>;
   constexpr int DT = T::DT, NU = T::NU;
   extern __shared__ __align__(512) char attn_smem[];
   char *const smem = attn_smem;
@@ -1474,7 +1474,7 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
   const int len = length_of(a, b);
   const int all = (a.Sk + 31) / 32;
   const int t0 = (int)((int64_t)all * split / a.splits), t1 = (int)((int64_t)all * (split + 1) / a.splits);
-  const int nrb = a.R > 32 ? 2 : 1;
+  const int nrb = (a.R + 31) / 32;
   const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
   const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
   const int rowlane = T::rowlane(lane), collane = T::collane(lane), col32 = T32::collane(lane);
@@ -1500,7 +1500,7 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
     mg.cut(a.D, tid);
     mq.store(smem + F::Q, tid);
     mg.store(smem + F::G, tid);
-    if (wave < F::NRB) {
+    if (wave < F::NRB) {  // (at most four)
       u32x4 gf[NU];
       const int r = wave * 32 + l31;
       load_rows<Tag, DP, VEC>(a, a.dout, b, hk, r, lane, gf);
@@ -1687,7 +1687,12 @@ hipError_t launch_bwd(const AttnArgs &a, hipStream_t stream) {
   const int64_t bh = a.B * a.Hk;
   if constexpr (Tag::W16) {
     if (a.one_pass) {
-      WBMM_ATTN_LAUNCH((attn_rows_bwd_kernel<Tag, DP, VEC>), bh * a.splits, (RowsShape<Tag, DP>::LDS), a);
+      // (blocks of 32 rows: as the registers allow, one_pass_rows)
+      constexpr int NRB = one_pass_rows(DP) / 32;
+      if (NRB == 4 && a.R <= 64)
+        WBMM_ATTN_LAUNCH((attn_rows_bwd_kernel<Tag, DP, 2, VEC>), bh * a.splits, (RowsShape<Tag, DP, 2>::LDS), a);
+      else
+        WBMM_ATTN_LAUNCH((attn_rows_bwd_kernel<Tag, DP, NRB, VEC>), bh * a.splits, (RowsShape<Tag, DP, NRB>::LDS), a);
       if (a.splits > 1) {
         const SumArgs s = {{a.part_o}, {a.dq}, bh * a.R, a.splits, a.R, a.G, a.Hk, a.D};
         WBMM_ATTN_LAUNCH((attn_sum_kernel<Tag>), (bh * a.R * a.D + 255) / 256, 0, s);

@@ -177,7 +177,7 @@ Space forward_space(const AttnArgs &a) {
 Space backward_space(const AttnArgs &a) {
   Space w = {};
   // dq's partial sums are spent before those of dk and dv are written
-  w.part_o = w.part_dk = up16(a.B * a.Hk * (int64_t)a.R * 8);
+  w.part_o = w.part_dk = a.one_pass ? 0 : up16(a.B * a.Hk * (int64_t)a.R * 8);
   const int64_t dq = a.splits > 1 ? up16((int64_t)a.splits * a.B * a.Hk * a.R * a.D * 4) : 0;
   const int64_t part = a.row_parts > 1 ? up16((int64_t)a.row_parts * a.B * a.Hk * a.Sk * a.D * 4) : 0;
   w.part_dv = w.part_dk + part;
@@ -364,20 +364,23 @@ void attn_plan_forward(Dt, AttnArgs *a) {
   a->row_parts = 1;
 }
 
-// dk and dv: the rows in parts only where the states' tiles leave most of the
-// chip idle, of at least 512 rows (float32, whose products take sixteen times
-// as long: 128), since the parts are summed by a launch of its own: one key
-// head of 16384 rows and 64 states takes 402 us in one part and 37 in 32, 8 heads
-// of 256 rows and 784 states 40 us in one and 47 in two.
+// Few rows (16-bit): all gradients in one pass over the states, whose parts
+// follow the same measure: 64 key heads of 128 components over 3136 states
+// 114 us in one part, 49 in four (one workgroup a unit), 60 in eight; 192
+// heads 24 us in one part, 26 in two.
+// Otherwise dk and dv take the rows in parts only where the states' tiles
+// leave most of the chip idle, of at least 512 rows (float32, whose products
+// take sixteen times as long: 128), since the parts are summed by a launch of
+// its own: one key head of 16384 rows and 64 states takes 402 us in one part and
+// 37 in 32, 8 heads of 256 rows and 784 states 40 us in one and 47 in two.
 void attn_plan_backward(Dt dt, AttnArgs *a) {
   plan_rows(a);
-  if (dt != Dt::F32 && a->R > 0 && a->R <= (a->D <= 64 ? 64 : 32) && a->Sk > 0) {
+  const int64_t bh = a->B * a->Hk, wgs = bh * cdiv(a->Sk, 128);
+  if (dt != Dt::F32 && a->R > 0 && a->R <= one_pass_rows(a->D) && a->Sk > 0) {
     a->one_pass = a->row_parts = 1;
-    const int64_t bh = a->B * a->Hk;
-    a->splits = (int)clamp(bh > 0 ? 2 * kUnits / bh : 1, 1, clamp(cdiv(a->Sk, 256), 1, 64));
+    a->splits = (int)clamp(bh > 0 ? kUnits / bh : 1, 1, clamp(a->Sk / 96, 1, 64));
     return;
   }
-  const int64_t wgs = a->B * a->Hk * cdiv(a->Sk, 128);
   a->row_parts = (int)clamp(wgs > 0 ? kUnits / wgs : 1, 1, clamp(a->R / (dt == Dt::F32 ? 128 : 512), 1, 64));
 }
 

@@ -63,6 +63,14 @@ struct AttnArgs {
   float *part_dk, *part_dv;
 };
 
+// Rows of a key head whose gradients are taken in one pass over the states
+// (16-bit), for heads of D components: dq of all rows is held in registers
+// beside dk and dv of a block.  Twice the rows need the registers of two waves
+// or spill, and were slower: 1024 heads of 128 components, 64 rows, 784 states
+// 772 us against 333 in separate kernels; 64 components, 128 rows 203 against 202;
+// 32 components, 100 rows 69 against 99.
+constexpr int one_pass_rows(int D) { return D <= 32 ? 128 : D <= 64 ? 64 : 32; }
+
 template <class Tag>
 struct AttnEntry {
   // VEC: rows of all tensors are whole 16-byte pieces

@@ -61,7 +61,8 @@ def test_rotary_refusals(lib, fn):
 
 
 def attention(lib, fn="forward", size=False, **kw):
-    p = dict(B=2, Sq=3, Sk=5, Hq=8, Hk=4, D=64, scale=0.125, dtype=1, lse=20 * FAR, lens=0, mask=0, mask_b=5, mask_s=1,
+    # (float32 gradients need a workspace for the rows' statistics)
+    p = dict(B=2, Sq=3, Sk=5, Hq=8, Hk=4, D=64, scale=0.125, dtype=0 if fn == "backward" else 1, lse=20 * FAR, lens=0, mask=0, mask_b=5, mask_s=1,
              ws=21 * FAR, ws_bytes=1 << 30)
     names = ("q", "k", "v", "out", "dout", "dq", "dk", "dv")
     p.update({k: v for k, v in kw.items() if k not in names})
@@ -130,8 +131,9 @@ def test_attention_workspace_query(lib):
     assert need > 0 and need % (8 * 129 * 4) == 0
     assert attention(lib, "forward", ws=0, **long) == E
     assert attention(lib, "forward", ws_bytes=need - 16, **long) == E
-    # a row's statistics: two float32 values
-    assert attention(lib, "backward", size=True, B=64, Sq=64, Sk=4096, Hq=16, Hk=16) == 64 * 64 * 16 * 8
+    # a row's statistics: two float32 values; none where one kernel does it all
+    assert attention(lib, "backward", size=True, dtype=1, B=64, Sq=128, Sk=4096, Hq=16, Hk=16) == 64 * 128 * 16 * 8
+    assert attention(lib, "backward", size=True, dtype=1, B=64, Sq=64, Sk=4096, Hq=16, Hk=16) == 0
 
 
 def test_binding_refusals():
