@@ -387,12 +387,13 @@ struct StateMover : Mover<Tag, DP, ROWS, THREADS> {
 // assembly because the compiler, which cannot tell the two halves of the
 // double buffer apart, would wait for the loads of the next tile before each
 // read of the present one.  `lds` is the wave's first byte; lane l's piece goes
-// 16 l bytes behind it.
+// 16 l bytes behind it.  The pause covers a base or M0 that a vector instruction
+// wrote just before (five wait states), which the compiler cannot see to.
 __device__ inline void lds_load16(uint32_t lds, const char *base, uint32_t offset) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(offset), "s"(base) : "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(lds), "v"(offset), "s"(base) : "m0");
 }
 __device__ inline void lds_load16(uint32_t lds, const char *at) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(at) : "m0");
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(lds), "v"(at) : "m0");
 }
 // The wave's loads have arrived (a barrier then tells the others).
 __device__ inline void lds_loads_done() { asm volatile("s_waitcnt vmcnt(0)" : : : "memory"); }
@@ -1567,6 +1568,11 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
         cols_product<Tag, DP>(smem, kt + collane, 0, wq, dq[rb]);
         wave_lds_fence();
       }
+      if (hide && !((see >> l31) & 1)) {
+        // a hidden state's column is its own, whatever the rows hold
+#pragma unroll
+        for (int d = 0; d < DT; ++d) dk[d] = dv[d] = (f32x16){};
+      }
     }
     auto row = [&](const Tokens &o, int n) {
       return j0 + n < a.Sk ? o.p + b * o.b + (j0 + n) * o.s + hk * o.h : nullptr;
@@ -1649,15 +1655,12 @@ __global__ __launch_bounds__(256) void attn_sum_kernel(SumArgs a) {
 
 // ---------------------------------------------------------------- launchers
 
-constexpr int64_t kMaxGrid = 1 << 23;  // workgroups of 256 threads in a launch
-
-#define WBMM_ATTN_LAUNCH(kernel, n, lds, args)                       \
-  do {                                                               \
-    const int64_t n_ = (n);                                          \
-    if (n_ > kMaxGrid) return hipErrorInvalidConfiguration;          \
-    kernel<<<dim3((unsigned)n_), dim3(256), (lds), stream>>>(args);  \
-    const hipError_t e_ = hipGetLastError();                         \
-    if (e_ != hipSuccess) return e_;                                 \
+// (the front end has checked the grids, attn_grids_fit)
+#define WBMM_ATTN_LAUNCH(kernel, n, lds, args)                               \
+  do {                                                                       \
+    kernel<<<dim3((unsigned)(n)), dim3(256), (lds), stream>>>(args);         \
+    const hipError_t e_ = hipGetLastError();                                 \
+    if (e_ != hipSuccess) return e_;                                         \
   } while (0)
 
 // Tiles of states can go straight to LDS.
@@ -1725,7 +1728,6 @@ hipError_t launch_bwd(const AttnArgs &a, hipStream_t stream) {
   if (a.row_parts > 1) {
     const SumArgs s = {{a.part_dk, a.part_dv}, {a.dk, a.dv}, bh * a.Sk, a.row_parts, a.Sk, 1, a.Hk, a.D};
     const int64_t n = (bh * a.Sk * a.D + 255) / 256;
-    if (n > kMaxGrid) return hipErrorInvalidConfiguration;
     attn_sum_kernel<Tag><<<dim3((unsigned)n, 2), dim3(256), 0, stream>>>(s);
     return hipGetLastError();
   }

@@ -28,8 +28,9 @@ wbmm_status from_hip(hipError_t e) {
 // Addresses that a strided [B, S, H, D] tensor reaches, in bytes.
 struct Span {
   uintptr_t at;
-  int64_t bytes;           // of the whole range
-  int64_t b, s, token;     // strides of entries and tokens, range of one token
+  int64_t bytes;                // of the whole range
+  int64_t row;                  // of one row of components
+  int64_t stride[3], n[3];      // entries, tokens, heads (stride 0: one of them)
 };
 
 constexpr int64_t kFar = (int64_t)1 << 46;  // bytes; keeps every offset far from overflow
@@ -50,7 +51,7 @@ bool describe(const wbmm_tokens &t, int64_t B, int64_t S, int64_t H, int64_t D, 
   if (!empty && (!t.data || !aligned(t.data, (size_t)es))) return false;
   // a stride over a single element is never taken
   *out = {(char *)t.data, B > 1 ? st[0] * es : 0, S > 1 ? st[1] * es : 0, H > 1 ? st[2] * es : 0};
-  *sp = {(uintptr_t)t.data, empty ? 0 : far * es, out->b, out->s, ((H - 1) * (H > 1 ? st[2] : 0) + D) * es};
+  *sp = {(uintptr_t)t.data, empty ? 0 : far * es, D * es, {out->b, out->s, out->h}, {B, S, H}};
   return true;
 }
 
@@ -73,14 +74,29 @@ bool folds(const Tokens &t, int64_t B, int64_t S, int64_t H, int64_t D, int64_t 
   return false;
 }
 
+// What lies below the period p: the range of the dimensions with smaller
+// strides; -1 if a larger stride is not a multiple of p.
+int64_t within(const Span &x, int64_t p) {
+  int64_t r = x.row;
+  for (int i = 0; i < 3; ++i) {
+    if (x.stride[i] >= p && x.stride[i] % p != 0) return -1;
+    if (x.stride[i] < p) r += x.stride[i] * (x.n[i] - 1);
+  }
+  return r;
+}
+
 bool clash(const Span &a, const Span &b) {
   if (a.bytes == 0 || b.bytes == 0) return false;
   if (a.at + (uintptr_t)a.bytes <= b.at || b.at + (uintptr_t)b.bytes <= a.at) return false;
-  // slices of one joint tensor: tokens at the same distances, separate parts
-  if (a.s == b.s && a.s > 0 && (a.b == 0 || a.b % a.s == 0) && (b.b == 0 || b.b % b.s == 0)) {
-    const int64_t d = (int64_t)((b.at - a.at) % (uintptr_t)a.s);
-    const int64_t shift = b.at >= a.at ? d : (int64_t)((a.s - (int64_t)((a.at - b.at) % (uintptr_t)a.s)) % a.s);
-    if (shift >= a.token && shift + b.token <= a.s) return false;
+  // slices of one joint tensor: apart within a period that both repeat by
+  for (int i = 0; i < 6; ++i) {
+    const int64_t p = i < 3 ? a.stride[i] : b.stride[i - 3];
+    if (p <= 0) continue;
+    const int64_t ra = within(a, p), rb = within(b, p);
+    if (ra < 0 || rb < 0) continue;
+    const int64_t m = b.at >= a.at ? (int64_t)((b.at - a.at) % (uintptr_t)p) : (int64_t)((a.at - b.at) % (uintptr_t)p);
+    const int64_t shift = b.at >= a.at || m == 0 ? m : p - m;  // of b behind a
+    if (shift >= ra && shift + rb <= p) return false;
   }
   return true;
 }
@@ -118,8 +134,8 @@ wbmm_status rotary(const wbmm_rotary_args *g, void *stream, int reverse) {
     if (n[i] > 1 && st[i] > kFar / (n[i] - 1)) return WBMM_ERR_INVALID_ARG;
     far += st[i] * (n[i] - 1);
   }
-  const Span pos = {(uintptr_t)g->positions, far * g->position_bytes, 0, 0, 0};
-  const Span fr = {(uintptr_t)g->freqs, pairs * 4, 0, 0, 0};
+  const Span pos = {(uintptr_t)g->positions, far * g->position_bytes, far * g->position_bytes, {}, {}};
+  const Span fr = {(uintptr_t)g->freqs, pairs * 4, pairs * 4, {}, {}};
   if (clash(y, pos) || clash(y, fr)) return WBMM_ERR_INVALID_ARG;
   a.pos = g->positions;
   a.pos_a = g->pos_stride_a, a.pos_b = g->pos_stride_b, a.pos_s = g->pos_stride_s;
@@ -197,7 +213,7 @@ bool clash_any(const Span &o, const Span *in, int n) {
   return false;
 }
 
-Span flat(const void *p, int64_t bytes) { return {(uintptr_t)p, p ? bytes : 0, 0, 0, 0}; }
+Span flat(const void *p, int64_t bytes) { return {(uintptr_t)p, p ? bytes : 0, bytes, {}, {}}; }
 
 // lens, mask and workspace as address ranges.
 void side_spans(const wbmm_cross_attention_args *g, Span *sp) {
@@ -254,6 +270,7 @@ wbmm_status wbmm_cross_attention_forward(const wbmm_cross_attention_args *g, voi
     return WBMM_ERR_INVALID_ARG;
   if (g->B == 0 || g->Sq == 0) return WBMM_OK;
   wbmm::attn_plan_forward((Dt)g->dtype, &a);
+  if (!wbmm::attn_grids_fit(a, false)) return WBMM_ERR_UNSUPPORTED;
   const Space w = forward_space(a);
   if (w.total > 0) {
     const Span ws = flat(g->workspace, w.total);
@@ -301,6 +318,7 @@ wbmm_status wbmm_cross_attention_backward(const wbmm_cross_attention_args *g, vo
   if (clash(out[0], out[1]) || clash(out[0], out[2]) || clash(out[1], out[2])) return WBMM_ERR_INVALID_ARG;
   if (g->B == 0 || (g->Sq == 0 && g->Sk == 0)) return WBMM_OK;
   wbmm::attn_plan_backward((Dt)g->dtype, &a);
+  if (!wbmm::attn_grids_fit(a, true)) return WBMM_ERR_UNSUPPORTED;
   const Space w = backward_space(a);
   if (w.total > 0) {
     const Span ws = flat(g->workspace, w.total);
@@ -382,6 +400,17 @@ void attn_plan_backward(Dt dt, AttnArgs *a) {
     return;
   }
   a->row_parts = (int)clamp(wgs > 0 ? kUnits / wgs : 1, 1, clamp(a->R / (dt == Dt::F32 ? 128 : 512), 1, 64));
+}
+
+bool attn_grids_fit(const AttnArgs &a, bool back) {
+  constexpr int64_t most = 1 << 23;  // workgroups of 256 threads in a launch
+  const int64_t bh = a.B * a.Hk, rows = bh * a.R;
+  // (bh is at most 2^30, the tiles of a head fewer: no overflow)
+  if (bh * cdiv(a.R, a.one_pass ? 1 << 30 : a.tile_rows) * a.splits > most) return false;
+  if (a.splits > 1 && rows > most * 256 / a.D) return false;
+  if (!back) return true;
+  if (!a.one_pass && bh * cdiv(a.Sk, 128) > most / a.row_parts) return false;
+  return a.row_parts == 1 || bh * a.Sk <= most * 256 / a.D;
 }
 
 }  // namespace wbmm

@@ -81,5 +81,7 @@ struct AttnEntry {
 // Tiles and parts of a call (functions of its sizes alone).
 void attn_plan_forward(Dt dt, AttnArgs *a);
 void attn_plan_backward(Dt dt, AttnArgs *a);
+// Whether every launch of a planned call is within the grid's limits.
+bool attn_grids_fit(const AttnArgs &a, bool back);
 
 }  // namespace wbmm

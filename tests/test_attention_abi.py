@@ -56,6 +56,8 @@ def test_rotary_refusals(lib, fn):
     assert call(y=dense(8 * FAR, 5, 4, 16)) == E and call(y=dense(9 * FAR, 5, 4, 16)) == E
     # one tensor, other strides: not in place
     assert call(x=(FAR, 320, 64, 16), y=(FAR, 320, 16, 80)) == E
+    # too many tokens for a launch
+    assert call(B=1 << 14, S=1 << 14, H=64, D=128, x=(FAR, 0, 0, 0), y=(1 << 44, (1 << 14) * 8192, 8192, 128)) == U
     # nothing to do
     assert call(B=0) == OK and call(S=0, x=(0, 0, 64, 16), y=(0, 0, 64, 16)) == OK
 
@@ -120,6 +122,42 @@ def test_attention_refusals(lib, fn):
     else:
         assert call(Sq=0) == OK
     assert call(B=0) == OK
+    # more tiles than a launch holds (broadcast inputs; outputs far apart)
+    wide = {n: ((8 + i) << 41, 0, 0, 0) for i, n in enumerate(("q", "k", "v", "dout"))}
+    wide["dk"], wide["dv"] = (30 << 41, 1 << 30, 1, 0), (31 << 41, 1 << 30, 1, 0)
+    if fn == "forward":
+        assert call(B=1, Sq=1 << 29, Sk=1, Hq=4, Hk=4, D=1, **{**wide, "out": (20 << 41, 0, 4, 1)}) == U
+    else:
+        assert call(B=2, Sq=1, Sk=1 << 30, Hq=1, Hk=1, D=1, **{**wide, "out": (20 << 41, 1, 0, 0), "dq": (21 << 41, 1, 0, 0)},
+                    ws=40 << 41, ws_bytes=1 << 40) == U
+
+
+def slices(lib, fn, B, S, H, D, order, first, second):
+    """A rotary call from one slice of a joint bfloat16 tensor to another that
+    fails on its positions alone, if not on the slices."""
+    if order == "bshd":
+        strides = (S * 3 * H * D, 3 * H * D, D)
+        at = lambda i: FAR + int(2 * i * H * D)
+    else:  # [B, 3 H, S, D]
+        strides = (3 * H * S * D, D, S * D)
+        at = lambda i: FAR + int(2 * i * H * S * D)
+    kw = dict(B=B, S=S, H=H, D=D, sections=(2,), axes=1)
+    clash = rotary(lib, fn, x=(at(first),) + strides, y=(at(second),) + strides, **kw) == E
+    return clash
+
+
+@pytest.mark.parametrize("order", ["bshd", "bhsd"])
+@pytest.mark.parametrize("B,S", [(2, 5), (8, 1), (1, 7)])
+def test_slices_of_one_tensor(lib, order, B, S):
+    """Slices that are apart pass the overlap check in every order (the calls
+    then fail on the launch, there being no GPU); ones that meet do not."""
+    if torch.cuda.is_available():
+        pytest.skip("would launch")
+    fn = "wbmm_rotary_forward"
+    assert not slices(lib, fn, B, S, 4, 16, order, 0, 1)
+    assert not slices(lib, fn, B, S, 4, 16, order, 2, 0)
+    assert slices(lib, fn, B, S, 4, 16, order, 0, 0.5)
+    assert slices(lib, fn, B, S, 4, 16, order, 1, 0.75)
 
 
 def test_attention_workspace_query(lib):

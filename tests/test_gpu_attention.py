@@ -397,6 +397,24 @@ def test_attention_nan_stays_in_its_row():
     assert bool(out[bad].isnan().all()) and torch.equal(out[~bad], clean[~bad])
 
 
+@pytest.mark.parametrize("Sq,Hq,D", [(3, 4, 32), (60, 2, 64), (40, 2, 128), (150, 2, 64)])
+def test_attention_nan_rows_leave_hidden_states_alone(Sq, Hq, D):
+    """Rows that hold NaN poison the gradients of what they see; hidden
+    states' gradients are zero all the same, and other rows' are untouched."""
+    q, k, v, g = (t.cuda() for t in attention_inputs(2, Sq, 90, Hq, 2, D, "bf16", seed=65))
+    mask = torch.rand(2, 90, generator=torch.Generator().manual_seed(66)).cuda() < 0.5
+    out, lse = W.wbmm_cross_attention_forward(q, k, v, key_mask=mask)
+    clean = W.wbmm_cross_attention_backward(g, q, k, v, out, lse, key_mask=mask)
+    q[1, 2, 0], g[1, 1, Hq - 1] = float("nan"), float("nan")
+    out, lse = W.wbmm_cross_attention_forward(q, k, v, key_mask=mask)
+    dq, dk, dv = W.wbmm_cross_attention_backward(g, q, k, v, out, lse, key_mask=mask)
+    assert bool((dk[~mask] == 0).all()) and bool((dv[~mask] == 0).all())
+    rows = torch.ones(2, Sq, Hq, dtype=torch.bool, device="cuda")
+    rows[1, 2, 0] = rows[1, 1, Hq - 1] = False
+    assert torch.equal(dq[rows], clean[0][rows]) and bool(dq[~rows].isnan().all())
+    assert torch.equal(dk[0], clean[1][0]) and torch.equal(dv[0], clean[2][0])
+
+
 def test_attention_long_cache_offsets():
     """States that lie more than 2^32 bytes into their tensor."""
     B, Sk, H, D = 2, 700, 2, 64
