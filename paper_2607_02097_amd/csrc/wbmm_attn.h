@@ -778,13 +778,14 @@ __global__ __launch_bounds__(256, Tag::W16 || DP <= 64 ? 2 : 1) void attn_few_ke
     f32x16 s = {};
 #pragma unroll
     for (int u = 0; u < T::NU; ++u) s = mma_chunk<Tag>(kf[u], qf[u], s);
-    const bool more = t + 4 < t1;
-    if (more) load_states<Tag, DP, VEC>(kb, a.k.s, (t + 4) * 32, len, a.D, lane, kf);
     uint32_t see = 0xffffffffu;
     if (mask || (t + 1) * 32 > len) see = (uint32_t)sight_bits(sight, t * 32, 32, len, lane);
     mv.hide(mask != nullptr, see, a.D, lane);
     mv.store(smem + vt, lane);
-    if (more) {
+    // (the next block's loads leave behind the last use of this one's: where
+    // they may or may not have left, a wait would have to take them in)
+    if (t + 4 < t1) {
+      load_states<Tag, DP, VEC>(kb, a.k.s, (t + 4) * 32, len, a.D, lane, kf);
       mv.load(vb, a.v.s, (t + 4) * 32, len, a.D, lane);
       sight = load_sight(mask, a.mask_s, (t + 4) * 32, 32, len, lane);
     }
@@ -1157,7 +1158,6 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_few_dq_kernel(Attn
     sight = load_sight(mask, a.mask_s, t * 32, 32, len, lane);
   }
   for (; t < t1; t += 4) {
-    const bool more = t + 4 < t1;
     uint32_t see = 0xffffffffu;
     if (mask || (t + 1) * 32 > len) see = (uint32_t)sight_bits(sight, t * 32, 32, len, lane);
     if (mask && !((see >> l31) & 1)) {
@@ -1170,10 +1170,10 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_few_dq_kernel(Attn
       s = mma_chunk<Tag>(kf[u], qf[u], s);
       *(u32x4 *)(smem + ((kt + rowlane) ^ (u << 5))) = kf[u];
     }
-    if (more) load_states<Tag, DP, VEC>(kb, a.k.s, (t + 4) * 32, len, a.D, lane, kf);
 #pragma unroll
     for (int u = 0; u < T::NU; ++u) dp = mma_chunk<Tag>(vf[u], gf[u], dp);
-    if (more) {
+    if (t + 4 < t1) {
+      load_states<Tag, DP, VEC>(kb, a.k.s, (t + 4) * 32, len, a.D, lane, kf);
       load_states<Tag, DP, VEC>(vb, a.v.s, (t + 4) * 32, len, a.D, lane, vf);
       sight = load_sight(mask, a.mask_s, (t + 4) * 32, 32, len, lane);
     }
