@@ -626,3 +626,11 @@ def test_layer_of_both_operators(dtype):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(caught, eager))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D,Sk", [(32, 100), (64, 470), (96, 200), (128, 64), (128, 330)])
+def test_attention_a_tile_for_each_unit(Sk, D, dtype):
+    """Tiles of 128 rows, about one for each compute unit, of one to eight
+    tiles of states, the last one partial, straight to LDS."""
+    run_and_check(*attention_inputs(25, 128, Sk, 8, 8, D, dtype, seed=150), dtype)
