@@ -107,10 +107,10 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a, RotPl
   const int ntok = left < pl.tok ? (int)left : pl.tok;
   const int h0 = blockIdx.y * pl.heads;
   const int nh = a.H - h0 < pl.heads ? a.H - h0 : pl.heads;
-  if (tid < ntok) {
-    const int64_t n = n0 + tid, b = pl.small ? (int64_t)((uint32_t)n / (uint32_t)a.S) : n / a.S, s = n - b * a.S;
-    at[2 * tid] = b * a.x.b + s * a.x.s;
-    at[2 * tid + 1] = b * a.y.b + s * a.y.s;
+  for (int t = tid; t < ntok; t += kRotThreads) {  // (up to 1024 tokens of one pair)
+    const int64_t n = n0 + t, b = pl.small ? (int64_t)((uint32_t)n / (uint32_t)a.S) : n / a.S, s = n - b * a.S;
+    at[2 * t] = b * a.x.b + s * a.x.s;
+    at[2 * t + 1] = b * a.y.b + s * a.y.s;
   }
   __syncthreads();
   const int per_token = nh * pl.per, items = ntok * per_token;

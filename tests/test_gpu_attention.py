@@ -106,6 +106,15 @@ def test_rotary(B, S, H, D, sections, adjacent, dtype):
         assert torch.equal(got[..., 2 * P:].cpu(), x[..., 2 * P:])
 
 
+@pytest.mark.parametrize("H,D,S", [(1, 2, (1 << 20) + 3), (2, 2, (1 << 19) + 1), (1, 4, (1 << 19) + 700)])
+def test_rotary_many_narrow_tokens(H, D, S):
+    """More tokens in a workgroup than it has threads."""
+    x, pos, freqs = draw((1, S, H, D), "bf16", 12), positions(1, 1, S, 13), W.wbmm_rotary_frequencies((1,), device="cpu")
+    want, mag = rotary_plain(x, pos, freqs, (1,), False)
+    got = W.wbmm_rotary_forward(x.cuda(), pos.cuda(), freqs.cuda(), (1,))
+    check(got, want, U["bf16"] * want.abs() + 2.0 ** -21 * mag, "bf16", "narrow")
+
+
 @pytest.mark.parametrize("offset", [0, 1, 2])
 def test_rotary_layouts(offset):
     """A slice of a joint projection (offset: unaligned by so many elements),
