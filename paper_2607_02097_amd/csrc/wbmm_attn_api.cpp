@@ -249,7 +249,7 @@ size_t wbmm_cross_attention_forward_workspace_bytes(const wbmm_cross_attention_a
   AttnArgs a;
   if (attn_sizes(g, &a) != WBMM_OK) return 0;
   wbmm::attn_plan_forward((Dt)g->dtype, &a);
-  return (size_t)forward_space(a).total;
+  return wbmm::attn_grids_fit(a, false) ? (size_t)forward_space(a).total : 0;
 }
 
 wbmm_status wbmm_cross_attention_forward(const wbmm_cross_attention_args *g, void *stream) {
@@ -289,7 +289,7 @@ size_t wbmm_cross_attention_backward_workspace_bytes(const wbmm_cross_attention_
   AttnArgs a;
   if (attn_sizes(g, &a) != WBMM_OK) return 0;
   wbmm::attn_plan_backward((Dt)g->dtype, &a);
-  return (size_t)backward_space(a).total;
+  return wbmm::attn_grids_fit(a, true) ? (size_t)backward_space(a).total : 0;
 }
 
 wbmm_status wbmm_cross_attention_backward(const wbmm_cross_attention_args *g, void *stream) {

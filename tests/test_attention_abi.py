@@ -163,6 +163,8 @@ def test_slices_of_one_tensor(lib, order, B, S):
 def test_attention_workspace_query(lib):
     assert attention(lib, "forward", size=True, dtype=9) == 0
     assert attention(lib, "backward", size=True, D=200) == 0
+    # nor does a call that is past the launch limits
+    assert attention(lib, "backward", size=True, B=1 << 15, Hq=1 << 15, Hk=1 << 15, Sq=1 << 30, Sk=1 << 30) == 0
     # one token over many states goes in parts; the parts' results take space
     long = dict(B=1, Sq=1, Sk=100000, Hq=8, Hk=8, D=128)
     need = attention(lib, "forward", size=True, **long)
