@@ -1566,7 +1566,7 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
           dp = mma_chunk<Tag>(*(const u32x4 *)(smem + ((F::G + rowlane) ^ x) + rb * 32 * F::PITCH),
                               *(const u32x4 *)(smem + ((vt + rowlane) ^ x)), dp);
         }
-        if (hide && !((see >> l31) & 1)) s = splat(-INFINITY);
+        if (hide && !((see >> l31) & 1)) s = splat(-INFINITY), dp = splat(0.f);
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           s[i] = exp2_(s[i] * a.c);

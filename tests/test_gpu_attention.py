@@ -424,6 +424,19 @@ def test_attention_nan_rows_leave_hidden_states_alone(Sq, Hq, D):
     assert torch.equal(dk[0], clean[1][0]) and torch.equal(dv[0], clean[2][0])
 
 
+@pytest.mark.parametrize("Sq,Hq,D", [(3, 4, 32), (60, 2, 64), (40, 2, 128), (150, 2, 64)])
+def test_attention_nan_gradient_where_nothing_is_visible(Sq, Hq, D):
+    """Rows that see nothing have no gradient, whatever comes from above."""
+    q, k, v, g = (t.cuda() for t in attention_inputs(2, Sq, 90, Hq, 2, D, "bf16", seed=67))
+    mask = torch.ones(2, 90, dtype=torch.bool, device="cuda")
+    mask[1] = False
+    g[1], q[1, 0] = float("nan"), float("nan")
+    out, lse = W.wbmm_cross_attention_forward(q, k, v, key_mask=mask)
+    assert bool((out[1] == 0).all()) and bool((lse[1] == -math.inf).all())
+    for t in W.wbmm_cross_attention_backward(g, q, k, v, out, lse, key_mask=mask):
+        assert bool((t[1] == 0).all()) and bool(t[0].isfinite().all())
+
+
 def test_attention_long_cache_offsets():
     """States that lie more than 2^32 bytes into their tensor."""
     B, Sk, H, D = 2, 700, 2, 64
