@@ -338,8 +338,8 @@ wbmm_status wbmm_rotary_backward(const wbmm_rotary_args *args, void *stream);
  * Where nothing is visible, out = 0, lse = -infinity and all gradients are 0;
  * gradients of states that are not visible are 0.
  * q, out, dout, dq: [B,Sq,Hq,D]; k, v, dk, dv: [B,Sk,Hk,D]; lse: float32
- * [B,Hq,Sq] contiguous.  1 <= D <= 128; scale positive and finite.  B, Sq
- * and Sk may be 0.  16-bit types: products on the matrix cores with float32
+ * [B,Hq,Sq] contiguous.  1 <= D <= 128; 1e-30 <= scale, finite.  B, Sq and
+ * Sk may be 0.  16-bit types: products on the matrix cores with float32
  * sums and a float32 softmax; p and its gradient are rounded to the type as
  * operands of the second products (float16: p's gradient has to be in the
  * type's range, as with any loss scale).  float32: float32 products.

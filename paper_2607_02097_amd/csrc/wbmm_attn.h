@@ -1711,10 +1711,12 @@ hipError_t launch_bwd(const AttnArgs &a, hipStream_t stream) {
     if (a.one_pass) {
       // (blocks of 32 rows: as the registers allow, one_pass_rows)
       constexpr int NRB = one_pass_rows(DP) / 32;
-      if (NRB == 4 && a.R <= 64)
-        WBMM_ATTN_LAUNCH((attn_rows_bwd_kernel<Tag, DP, 2, VEC>), bh * a.splits, (RowsShape<Tag, DP, 2>::LDS), a);
-      else
-        WBMM_ATTN_LAUNCH((attn_rows_bwd_kernel<Tag, DP, NRB, VEC>), bh * a.splits, (RowsShape<Tag, DP, NRB>::LDS), a);
+      bool half = false;
+      if constexpr (NRB == 4) {
+        half = a.R <= 64;
+        if (half) WBMM_ATTN_LAUNCH((attn_rows_bwd_kernel<Tag, DP, 2, VEC>), bh * a.splits, (RowsShape<Tag, DP, 2>::LDS), a);
+      }
+      if (!half) WBMM_ATTN_LAUNCH((attn_rows_bwd_kernel<Tag, DP, NRB, VEC>), bh * a.splits, (RowsShape<Tag, DP, NRB>::LDS), a);
       if (a.splits > 1) {
         const SumArgs s = {{a.part_o}, {a.dq}, bh * a.R, a.splits, a.R, a.G, a.Hk, a.D};
         WBMM_ATTN_LAUNCH((attn_sum_kernel<Tag>), (bh * a.R * a.D + 255) / 256, 0, s);

@@ -154,7 +154,8 @@ wbmm_status attn_sizes(const wbmm_cross_attention_args *g, AttnArgs *a) {
   if (!elem_size(g->dtype)) return WBMM_ERR_UNSUPPORTED;
   if (g->B < 0 || g->Sq < 0 || g->Sk < 0 || g->Hq <= 0 || g->Hk <= 0 || g->D <= 0) return WBMM_ERR_INVALID_ARG;
   if (g->Hq % g->Hk != 0) return WBMM_ERR_INVALID_ARG;
-  if (!(g->scale > 0) || !isfinite((float)g->scale) || (float)g->scale == 0.f) return WBMM_ERR_INVALID_ARG;
+  // (lse / scale has to be within float32's range)
+  if (!(g->scale >= 1e-30) || !isfinite((float)g->scale)) return WBMM_ERR_INVALID_ARG;
   if (g->D > wbmm::kMaxHeadDim) return WBMM_ERR_UNSUPPORTED;
   // rows of a key head and states are counted in 32 bits, with room to spare
   const int64_t lim = (int64_t)1 << 30, G = g->Hq / g->Hk;
@@ -168,7 +169,7 @@ wbmm_status attn_sizes(const wbmm_cross_attention_args *g, AttnArgs *a) {
   a->R = (int)(g->Sq * G);
   a->scale = (float)g->scale;
   a->c = (float)(g->scale * 1.4426950408889634074);
-  if (!isfinite(a->c) || a->c == 0.f) return WBMM_ERR_INVALID_ARG;
+  if (!isfinite(a->c)) return WBMM_ERR_INVALID_ARG;
   a->lens = g->kv_lens;
   a->mask = g->key_mask;
   a->mask_b = g->mask_stride_b, a->mask_s = g->mask_stride_s;

@@ -90,7 +90,7 @@ def test_attention_refusals(lib, fn):
     assert call(Hq=9) == E and call(Hk=0) == E and call(Hq=0) == E
     assert call(B=-1) == E and call(Sq=-1) == E and call(Sk=-1) == E
     assert call(Sq=1 << 30) == U and call(Sk=1 << 31) == U
-    for scale in (0.0, -1.0, float("inf"), float("nan"), 1e-60):
+    for scale in (0.0, -1.0, float("inf"), float("nan"), 1e-60, 1e-31, 3e38):
         assert call(scale=scale) == E, scale
     for n in ("q", "k", "v", "out") + (("dout", "dq", "dk", "dv") if fn == "backward" else ()):
         S, H = (5, 4) if n in ("k", "v", "dk", "dv") else (3, 8)

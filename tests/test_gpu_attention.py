@@ -656,3 +656,22 @@ def test_attention_a_tile_for_each_unit(Sk, D, dtype):
     """Tiles of 128 rows, about one for each compute unit, of one to eight
     tiles of states, the last one partial, straight to LDS."""
     run_and_check(*attention_inputs(25, 128, Sk, 8, 8, D, dtype, seed=150), dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("kind", ["", "lens+mask"])
+@pytest.mark.parametrize("Sq,D", [(40, 24), (50, 37), (64, 72), (33, 128), (100, 64), (65, 37), (128, 72), (90, 128)])
+def test_attention_tiles_of_64_and_128_rows(Sq, D, kind, dtype):
+    """As many heads as take whole tiles of rows, in rows of whole 16-byte
+    pieces and others, masked and not, two tiles of states."""
+    B, H, Sk = 48, 4, 77
+    lens, mask = hidden(B, Sk, kind)
+    run_and_check(*attention_inputs(B, Sq, Sk, 2 * H if Sq == 33 else H, H, D, dtype, seed=160), dtype, lens, mask)
+
+
+def test_attention_small_and_large_scales():
+    """Weights that are all alike, and one state that takes everything."""
+    for dtype in DT:
+        q, k, v, g = attention_inputs(2, 70, 50, 2, 2, 32, dtype, seed=170)
+        for scale in (1e-30, 1e-4, 16.0):
+            run_and_check(q, k, v, g, dtype, scale=scale, tag="scale %g" % scale)
