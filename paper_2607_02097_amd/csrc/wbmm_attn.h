@@ -54,12 +54,8 @@ struct Tile {
   static constexpr int LPC = PITCH / 16;                          // chunks of an LDS row
   static constexpr int NU = DP / (2 * CE);                        // chunk pairs of a row
   static constexpr int DT = DP / 32;
-  // The chunk of a row that belongs at a slot, for a load of whole rows (slots
-  // past the row, which nobody reads, take its first chunk).
-  __device__ static int chunk_at(int slot, int row) {
-    const int c = slot ^ swz(row);
-    return DP * ES < PITCH && c >= DP / CE ? 0 : c;
-  }
+  // The chunk of a row that belongs at a slot.
+  __device__ static int chunk_at(int slot, int row) { return slot ^ swz(row); }
   __device__ static int swz(int row) {
     if constexpr (ES == 2) {
       if constexpr (PITCH == 256) return ((row & 3) << 2) | ((row >> 2) & 3);
@@ -380,10 +376,13 @@ struct StateMover : Mover<Tag, DP, ROWS, THREADS> {
 
 // ----------------------------------------------- from memory straight to LDS
 //
-// Tiles whose rows are all visible and whole (no mask, D = DP) skip the
-// registers: each lane names the 16 bytes that belong at its place in LDS, so
-// the swizzle is in the choice of the chunk.  This frees the registers of the
-// tile in flight (32 of 256 in the forward at 128 components).  Written as
+// Tiles of whole 16-byte pieces skip the registers: each lane names the 16
+// bytes that belong at its place in LDS, so the swizzle is in the choice of the
+// chunk.  This frees the registers of the tile in flight (32 of 256 in the
+// forward at 128 components), and a head of 72 components, padded to 96, takes
+// less time than one of 128.  Lanes whose chunk lies past D do not load; their
+// places are zeroed once.  Rows that must not be seen are zeroed in LDS when
+// they have arrived, by the lanes that loaded them.  Written as
 // assembly because the compiler, which cannot tell the two halves of the
 // double buffer apart, would wait for the loads of the next tile before each
 // read of the present one.  `lds` is the wave's first byte; lane l's piece goes
@@ -402,19 +401,44 @@ __device__ inline uint32_t lds_offset(const char *p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)p;
 }
 
-// A tile of ROWS states by four waves.  Strides are below 2^24 bytes (the
-// launcher checks), so a lane's offset in a tile fits 32 bits.
+// Places of a thread in tiles of ROWS rows that four waves load.
 template <class Tag, int DP, int ROWS>
-struct DirectStates {
+struct DirectTile {
+  using M = Mover<Tag, DP, ROWS, 256>;
+  __device__ static bool has(int tid, int p, int D) {
+    // (the swizzle has a period of 16 rows)
+    return M::T::chunk_at(M::chunk(tid), M::row(tid, M::RPP % 16 == 0 ? 0 : p)) * M::T::CE < D;
+  }
+  // Zeroes the places past D of `tiles` tiles.
+  __device__ static void clear(char *tile, int tiles, int D, int tid) {
+    if (D == DP) return;
+#pragma unroll
+    for (int p = 0; p < M::NP; ++p)
+      if ((ROWS % M::RPP == 0 || M::row(tid, p) < ROWS) && !has(tid, p, D))
+        for (int n = 0; n < tiles; ++n) *(u32x4 *)(tile + n * ROWS * M::T::PITCH + p * 4096 + tid * 16) = (u32x4){0, 0, 0, 0};
+  }
+  // Zeroes the rows that must not be seen.
+  __device__ static void hide(char *tile, uint64_t see, int tid) {
+#pragma unroll
+    for (int p = 0; p < M::NP; ++p)
+      if (!((see >> (M::row(tid, p) & 63)) & 1)) *(u32x4 *)(tile + p * 4096 + tid * 16) = (u32x4){0, 0, 0, 0};
+  }
+};
+
+// A tile of ROWS states by four waves.  Strides are below 2^24 bytes (the
+// front end checks), so a lane's offset in a tile fits 32 bits.
+template <class Tag, int DP, int ROWS>
+struct DirectStates : DirectTile<Tag, DP, ROWS> {
   using M = Mover<Tag, DP, ROWS, 256>;
   static_assert(ROWS % M::RPP == 0, "whole passes");
-  __device__ static void load(uint32_t lds, const char *base, int64_t stride, int first, int end, int tid, int wave) {
+  __device__ static void load(uint32_t lds, const char *base, int64_t stride, int first, int end, int D, int tid, int wave) {
     const int c = M::chunk(tid);
     const char *tile = base + first * stride;
 #pragma unroll
     for (int p = 0; p < M::NP; ++p) {
       const int rw = M::row(tid, p), last = end - 1 - first, j = rw < last ? rw : last;
-      lds_load16(lds + p * 4096 + wave * 1024, tile, (uint32_t)j * (uint32_t)stride + (M::T::chunk_at(c, rw) << 4));
+      if (DirectTile<Tag, DP, ROWS>::has(tid, p, D))
+        lds_load16(lds + p * 4096 + wave * 1024, tile, (uint32_t)j * (uint32_t)stride + (M::T::chunk_at(c, rw) << 4));
     }
   }
 };
@@ -537,7 +561,7 @@ __device__ inline bool running_top(const f32x16 *s, float c, float *top, float *
 // ------------------------------------------------------------------ forward
 
 // A workgroup takes 32 (4 / WK) rows and runs over the states in tiles of BN,
-// double-buffered in LDS, the next tile on its way: straight to LDS (DIRECT) or
+// double-buffered in LDS, the next tile on its way: straight to LDS (VEC) or
 // in registers.  WK waves share 32 rows and split each tile's states, joined at
 // the end.  32 rows a wave leave room for two waves a SIMD, of two workgroups,
 // whose softmax and products overlap without further arrangement.
@@ -559,10 +583,11 @@ struct FwdShape {
   static constexpr int LDS = 4 * TILE;
 };
 
-template <class Tag, int DP, int WK, bool VEC, bool DIRECT>
+template <class Tag, int DP, int WK, bool VEC>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   using T = Tile<Tag, DP>;
   using F = FwdShape<Tag, DP, WK>;
+  using Direct = DirectStates<Tag, DP, F::BN>;
   constexpr int NB = F::NB, DT = T::DT;
   extern __shared__ __align__(512) char attn_smem[];
   char *const smem = attn_smem;
@@ -580,7 +605,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   u32x4 qf[T::NU];
   load_rows<Tag, DP, VEC>(a, a.q, b, hk, r, lane, qf);
   const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
-  const uint8_t *mask = !DIRECT && a.mask ? a.mask + b * a.mask_b : nullptr;
+  const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
   StateMover<Tag, DP, VEC, F::BN, 256> mk, mv;
   uint32_t sight = 1;
   const int rowlane = T::rowlane(lane), collane = T::collane(lane);
@@ -588,27 +613,30 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   f32x16 acc[DT] = {};
   float top = -INFINITY, sum = 0.f;
   auto load = [&](int t) {
-    if constexpr (DIRECT) {
+    sight = load_sight(mask, a.mask_s, t * F::BN, F::BN, len, lane);
+    if constexpr (VEC) {
       const uint32_t to = lds_offset(smem) + (t & 1) * 2 * F::TILE;
-      DirectStates<Tag, DP, F::BN>::load(to, kb, a.k.s, t * F::BN, len, tid, wave);
-      DirectStates<Tag, DP, F::BN>::load(to + F::TILE, vb, a.v.s, t * F::BN, len, tid, wave);
+      Direct::load(to, kb, a.k.s, t * F::BN, len, a.D, tid, wave);
+      Direct::load(to + F::TILE, vb, a.v.s, t * F::BN, len, a.D, tid, wave);
     } else {
       mk.load(kb, a.k.s, t * F::BN, len, a.D, tid);
       mv.load(vb, a.v.s, t * F::BN, len, a.D, tid);
-      sight = load_sight(mask, a.mask_s, t * F::BN, F::BN, len, lane);
     }
   };
+  if constexpr (VEC) Direct::clear(smem, 4, a.D, tid);
   if (t1 > 0) load(0);
   arrived(qf);
   for (int t = 0; t < t1; ++t) {
     const int kt = (t & 1) * 2 * F::TILE, vt = kt + F::TILE;
     uint64_t see = ~(uint64_t)0;
     if (mask || (t + 1) * F::BN > len) see = sight_bits(sight, t * F::BN, F::BN, len, lane);
-    if constexpr (DIRECT) {
+    const bool hide = see != ~(uint64_t)0;
+    if constexpr (VEC) {
       lds_loads_done();
+      if (hide) Direct::hide(smem + vt, see, tid);
     } else {
-      mk.hide(mask != nullptr, see, a.D, tid);
-      mv.hide(mask != nullptr, see, a.D, tid);
+      mk.hide(hide, see, a.D, tid);
+      mv.hide(hide, see, a.D, tid);
       mk.store(smem + kt, tid);
       mv.store(smem + vt, tid);
     }
@@ -616,7 +644,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
     if (t + 1 < t1) load(t + 1);
     f32x16 s[NB];
     rows_products<Tag, DP, NB, Tag::W16 ? 8 : 4>(smem, kt + rowlane, wk * F::KW, qf, s);
-    if (see != ~(uint64_t)0) {
+    if (hide) {
 #pragma unroll
       for (int k = 0; k < NB; ++k) {
         const uint32_t bits = (uint32_t)(see >> (wk * F::KW + 32 * k)) >> (4 * h);
@@ -993,10 +1021,11 @@ __device__ inline void to_ds(f32x16 *s, const f32x16 &dp, float c, float2 st, ui
 // states, WK waves sharing rows and splitting each tile.  Measured, bfloat16,
 // 8 x 32 heads of 512 queries over 3136 states of 128 components: 285 us for
 // three products, 1.1 PFLOP/s.
-template <class Tag, int DP, int WK, bool VEC, bool DIRECT>
+template <class Tag, int DP, int WK, bool VEC>
 __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs a) {
   using T = Tile<Tag, DP>;
   using F = FwdShape<Tag, DP, WK>;
+  using Direct = DirectStates<Tag, DP, F::BN>;
   constexpr int DT = T::DT, NB = F::NB;
   extern __shared__ __align__(512) char attn_smem[];
   char *const smem = attn_smem;
@@ -1013,22 +1042,23 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs
   load_rows<Tag, DP, VEC>(a, a.dout, b, hk, r, lane, gf);
   const float2 st = row_stat<Tag, DP, VEC>(a, b, hk, r, lane, gf, wk == 0);
   const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
-  const uint8_t *mask = !DIRECT && a.mask ? a.mask + b * a.mask_b : nullptr;
+  const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
   StateMover<Tag, DP, VEC, F::BN, 256> mk, mv;
   uint32_t sight = 1;
   const int rowlane = T::rowlane(lane), collane = T::collane(lane);
   f32x16 acc[DT] = {};
   auto load = [&](int t) {
-    if constexpr (DIRECT) {
+    sight = load_sight(mask, a.mask_s, t * F::BN, F::BN, len, lane);
+    if constexpr (VEC) {
       const uint32_t to = lds_offset(smem) + (t & 1) * 2 * F::TILE;
-      DirectStates<Tag, DP, F::BN>::load(to, kb, a.k.s, t * F::BN, len, tid, wave);
-      DirectStates<Tag, DP, F::BN>::load(to + F::TILE, vb, a.v.s, t * F::BN, len, tid, wave);
+      Direct::load(to, kb, a.k.s, t * F::BN, len, a.D, tid, wave);
+      Direct::load(to + F::TILE, vb, a.v.s, t * F::BN, len, a.D, tid, wave);
     } else {
       mk.load(kb, a.k.s, t * F::BN, len, a.D, tid);
       mv.load(vb, a.v.s, t * F::BN, len, a.D, tid);
-      sight = load_sight(mask, a.mask_s, t * F::BN, F::BN, len, lane);
     }
   };
+  if constexpr (VEC) Direct::clear(smem, 4, a.D, tid);
   if (t1 > 0) load(0);
   arrived(qf);
   arrived(gf);
@@ -1036,11 +1066,13 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs
     const int kt = (t & 1) * 2 * F::TILE, vt = kt + F::TILE;
     uint64_t see = ~(uint64_t)0;
     if (mask || (t + 1) * F::BN > len) see = sight_bits(sight, t * F::BN, F::BN, len, lane);
-    if constexpr (DIRECT) {
+    const bool hide = see != ~(uint64_t)0;
+    if constexpr (VEC) {
       lds_loads_done();
+      if (hide) Direct::hide(smem + kt, see, tid);
     } else {
-      mk.hide(mask != nullptr, see, a.D, tid);
-      mv.hide(mask != nullptr, see, a.D, tid);
+      mk.hide(hide, see, a.D, tid);
+      mv.hide(hide, see, a.D, tid);
       mk.store(smem + kt, tid);
       mv.store(smem + vt, tid);
     }
@@ -1051,11 +1083,11 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs
       const int base = wk * F::KW + 32 * k;
       f32x16 s = splat(kStart<Tag> ? st.x : 0.f), dp = splat(kStart<Tag> ? st.y : 0.f);
       const uint32_t seen = (uint32_t)(see >> base);
-      if constexpr (Tag::W16 && DIRECT) {
+      if constexpr (Tag::W16 && VEC) {
         // One stream of fragment reads, some products ahead of their use: keys
         // for the scores, values for dp (while which the weights are formed),
         // columns of the keys for dq.
-        constexpr int NU = T::NU, N = 2 * NU + 2 * DT, P0 = DIRECT ? 8 : 4, P = P0 < N ? P0 : N;
+        constexpr int NU = T::NU, N = 2 * NU + 2 * DT, P = 8 < N ? 8 : N;
         u32x4 f[P], w[2];
         auto read = [&](int n) {
           if (n < 2 * NU)
@@ -1274,7 +1306,7 @@ struct RowWalk {
       if constexpr (DIRECT) {
         const int c = M::T::chunk_at(M::chunk(tid), M::row(tid, p)) << 4;
         const uint32_t to = lds + p * 4096 + wave * 1024;
-        if (ROWS % M::RPP == 0 || wave * (M::RPP / 4) < ROWS) {
+        if ((ROWS % M::RPP == 0 || wave * (M::RPP / 4) < ROWS) && DirectTile<Tag, DP, ROWS>::has(tid, p, a.D)) {
           lds_load16(to, q + c);
           lds_load16(to + ROWS * M::T::PITCH, o + c);
         }
@@ -1295,7 +1327,7 @@ struct RowWalk {
   }
 };
 
-template <class Tag, int DP, bool VEC, bool DIRECT>
+template <class Tag, int DP, bool VEC>
 __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArgs a) {
   using T = Tile<Tag, DP>;
   using F = DkvShape<Tag, DP>;
@@ -1336,20 +1368,21 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
   const float2 blind = make_float2(kStart<Tag> ? kBlind : -kBlind, 0.f);
   float2 st = blind;
   auto load = [&](int t) {
-    walk.template load<DIRECT>(a, qb, gb, tid, &mq, &mg, lds_offset(smem) + (t & 1) * 2 * F::TILE, wave);
+    walk.template load<VEC>(a, qb, gb, tid, &mq, &mg, lds_offset(smem) + (t & 1) * 2 * F::TILE, wave);
     if (tid < F::BR) {
       st = blind;
       if (t * F::BR + tid < a.R) st = a.rowstat[bh * a.R + t * F::BR + tid];
     }
   };
   f32x16 dk[DT] = {}, dv[DT] = {};
+  if constexpr (VEC) DirectTile<Tag, DP, F::BR>::clear(smem, 4, a.D, tid);
   if (t0 < t1) load(t0);
   arrived(kf);
   if constexpr (!F::VLDS) arrived(vf);
   for (int t = t0; t < t1; ++t) {
     const int qt = (t & 1) * 2 * F::TILE, gt = qt + F::TILE;
     float *stat = (float *)(smem + F::STAT) + (t & 1) * 2 * F::BR;
-    if constexpr (DIRECT) {
+    if constexpr (VEC) {
       lds_loads_done();
     } else {
       mq.cut(a.D, tid);
@@ -1372,7 +1405,7 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
         for (int e = 0; e < 4; ++e) s[i + e] = x[e], dp[i + e] = y[e];
       }
     }
-    if constexpr (Tag::W16 && DIRECT && F::VLDS) {
+    if constexpr (Tag::W16 && VEC && F::VLDS) {
       // One stream of fragment reads, some products ahead of their use: queries
       // for the scores, do (and the values, where they are in LDS) for dp, while
       // which the weights are formed, then the columns of do and of the queries.
@@ -1682,12 +1715,6 @@ __global__ __launch_bounds__(256) void attn_sum_kernel(SumArgs a) {
     if (e_ != hipSuccess) return e_;                                         \
   } while (0)
 
-// Tiles of states can go straight to LDS.
-template <class Tag, int DP, bool VEC>
-bool states_direct(const AttnArgs &a) {
-  return VEC && !a.mask && a.D == DP && a.k.s < (1 << 24) && a.v.s < (1 << 24);
-}
-
 template <class Tag, int DP, bool VEC>
 hipError_t launch_fwd(const AttnArgs &a, hipStream_t stream) {
   const int64_t bh = a.B * a.Hk;
@@ -1695,11 +1722,9 @@ hipError_t launch_fwd(const AttnArgs &a, hipStream_t stream) {
     WBMM_ATTN_LAUNCH((attn_few_kernel<Tag, DP, VEC>), bh * ((a.R + 31) / 32) * a.splits, (FewShape<Tag, DP>::lds(a.R)), a);
     if (a.splits > 1) WBMM_ATTN_LAUNCH((attn_join_kernel<Tag>), (bh * a.R * a.D + 255) / 256, 0, a);
   } else if (a.tile_rows == 64) {
-    WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 2, VEC, false>), bh * ((a.R + 63) / 64), (FwdShape<Tag, DP, 2>::LDS), a);
-  } else if (states_direct<Tag, DP, VEC>(a)) {
-    WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 1, VEC, VEC>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
+    WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 2, VEC>), bh * ((a.R + 63) / 64), (FwdShape<Tag, DP, 2>::LDS), a);
   } else {
-    WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 1, VEC, false>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
+    WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 1, VEC>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
   }
   return hipSuccess;
 }
@@ -1733,19 +1758,14 @@ hipError_t launch_bwd(const AttnArgs &a, hipStream_t stream) {
         WBMM_ATTN_LAUNCH((attn_sum_kernel<Tag>), (bh * a.R * a.D + 255) / 256, 0, s);
       }
     } else if (a.tile_rows == 64) {
-      WBMM_ATTN_LAUNCH((attn_dq_kernel<Tag, DP, 2, VEC, false>), bh * ((a.R + 63) / 64), (FwdShape<Tag, DP, 2>::LDS), a);
-    } else if (states_direct<Tag, DP, VEC>(a)) {
-      WBMM_ATTN_LAUNCH((attn_dq_kernel<Tag, DP, 1, VEC, VEC>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
+      WBMM_ATTN_LAUNCH((attn_dq_kernel<Tag, DP, 2, VEC>), bh * ((a.R + 63) / 64), (FwdShape<Tag, DP, 2>::LDS), a);
     } else {
-      WBMM_ATTN_LAUNCH((attn_dq_kernel<Tag, DP, 1, VEC, false>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
+      WBMM_ATTN_LAUNCH((attn_dq_kernel<Tag, DP, 1, VEC>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
     }
   }
   if (a.Sk == 0) return hipSuccess;
   const int64_t n_dkv = bh * ((a.Sk + 127) / 128) * a.row_parts;
-  if (VEC && a.D == DP)
-    WBMM_ATTN_LAUNCH((attn_dkv_kernel<Tag, DP, VEC, VEC>), n_dkv, (DkvShape<Tag, DP>::LDS), a);
-  else
-    WBMM_ATTN_LAUNCH((attn_dkv_kernel<Tag, DP, VEC, false>), n_dkv, (DkvShape<Tag, DP>::LDS), a);
+  WBMM_ATTN_LAUNCH((attn_dkv_kernel<Tag, DP, VEC>), n_dkv, (DkvShape<Tag, DP>::LDS), a);
   if (a.row_parts > 1) {
     const SumArgs s = {{a.part_dk, a.part_dv}, {a.dk, a.dv}, bh * a.Sk, a.row_parts, a.Sk, 1, a.Hk, a.D};
     const int64_t n = (bh * a.Sk * a.D + 255) / 256;

@@ -208,6 +208,10 @@ bool rows16(const Tokens *const *t, int n, int64_t row) {
   return ok;
 }
 
+// Offsets in a tile of states fit 32 bits (states further apart are moved
+// element by element).
+bool near(const AttnArgs &a) { return a.k.s < (1 << 24) && a.v.s < (1 << 24); }
+
 bool clash_any(const Span &o, const Span *in, int n) {
   for (int i = 0; i < n; ++i)
     if (clash(o, in[i])) return true;
@@ -283,7 +287,7 @@ wbmm_status wbmm_cross_attention_forward(const wbmm_cross_attention_args *g, voi
   }
   a.lse = g->lse;
   const Tokens *t[] = {&a.q, &a.k, &a.v, &a.o};
-  return from_hip(run(g->dtype, a, rows16(t, 4, g->D * es), false, (hipStream_t)stream));
+  return from_hip(run(g->dtype, a, rows16(t, 4, g->D * es) && near(a), false, (hipStream_t)stream));
 }
 
 size_t wbmm_cross_attention_backward_workspace_bytes(const wbmm_cross_attention_args *g) {
@@ -333,7 +337,7 @@ wbmm_status wbmm_cross_attention_backward(const wbmm_cross_attention_args *g, vo
   }
   a.lse = g->lse;
   const Tokens *t[] = {&a.q, &a.k, &a.v, &a.o, &a.dout, &a.dq, &a.dk, &a.dv};
-  return from_hip(run(g->dtype, a, rows16(t, 8, g->D * es), true, (hipStream_t)stream));
+  return from_hip(run(g->dtype, a, rows16(t, 8, g->D * es) && near(a), true, (hipStream_t)stream));
 }
 
 }  // extern "C"
