@@ -401,24 +401,27 @@ __device__ inline uint32_t lds_offset(const char *p) {
   return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)p;
 }
 
-// Places of a thread in tiles of ROWS rows that four waves load.
-template <class Tag, int DP, int ROWS>
+// Places of a thread in tiles of ROWS rows that four waves load.  PLAIN: D = DP
+// and no mask, known ahead.
+template <class Tag, int DP, int ROWS, bool PLAIN>
 struct DirectTile {
   using M = Mover<Tag, DP, ROWS, 256>;
   __device__ static bool has(int tid, int p, int D) {
     // (the swizzle has a period of 16 rows)
-    return M::T::chunk_at(M::chunk(tid), M::row(tid, M::RPP % 16 == 0 ? 0 : p)) * M::T::CE < D;
+    return PLAIN || M::T::chunk_at(M::chunk(tid), M::row(tid, M::RPP % 16 == 0 ? 0 : p)) * M::T::CE < D;
   }
   // Zeroes the places past D of `tiles` tiles.
   __device__ static void clear(char *tile, int tiles, int D, int tid) {
-    if (D == DP) return;
+    if (PLAIN || D == DP) return;
 #pragma unroll
     for (int p = 0; p < M::NP; ++p)
       if ((ROWS % M::RPP == 0 || M::row(tid, p) < ROWS) && !has(tid, p, D))
         for (int n = 0; n < tiles; ++n) *(u32x4 *)(tile + n * ROWS * M::T::PITCH + p * 4096 + tid * 16) = (u32x4){0, 0, 0, 0};
   }
-  // Zeroes the rows that must not be seen.
+  // Zeroes the rows that must not be seen.  (Nothing of it is to be computed
+  // ahead of the loop and kept there.)
   __device__ static void hide(char *tile, uint64_t see, int tid) {
+    asm volatile("" : "+v"(tid));
 #pragma unroll
     for (int p = 0; p < M::NP; ++p)
       if (!((see >> (M::row(tid, p) & 63)) & 1)) *(u32x4 *)(tile + p * 4096 + tid * 16) = (u32x4){0, 0, 0, 0};
@@ -426,18 +429,22 @@ struct DirectTile {
 };
 
 // A tile of ROWS states by four waves.  Strides are below 2^24 bytes (the
-// front end checks), so a lane's offset in a tile fits 32 bits.
-template <class Tag, int DP, int ROWS>
-struct DirectStates : DirectTile<Tag, DP, ROWS> {
+// front end checks), so a lane's offset in a tile fits 32 bits.  ANEW: a lane's
+// places are worked out anew for each tile, where a kernel has no registers to
+// keep them in (the gradients: 128 components, 512 queries over 1001 masked
+// states 143 -> 135 us; the forward, which has: 790 -> 835 us).
+template <class Tag, int DP, int ROWS, bool PLAIN, bool ANEW>
+struct DirectStates : DirectTile<Tag, DP, ROWS, PLAIN> {
   using M = Mover<Tag, DP, ROWS, 256>;
   static_assert(ROWS % M::RPP == 0, "whole passes");
   __device__ static void load(uint32_t lds, const char *base, int64_t stride, int first, int end, int D, int tid, int wave) {
+    if constexpr (ANEW) asm volatile("" : "+v"(tid));
     const int c = M::chunk(tid);
     const char *tile = base + first * stride;
 #pragma unroll
     for (int p = 0; p < M::NP; ++p) {
       const int rw = M::row(tid, p), last = end - 1 - first, j = rw < last ? rw : last;
-      if (DirectTile<Tag, DP, ROWS>::has(tid, p, D))
+      if (DirectTile<Tag, DP, ROWS, PLAIN>::has(tid, p, D))
         lds_load16(lds + p * 4096 + wave * 1024, tile, (uint32_t)j * (uint32_t)stride + (M::T::chunk_at(c, rw) << 4));
     }
   }
@@ -583,11 +590,11 @@ struct FwdShape {
   static constexpr int LDS = 4 * TILE;
 };
 
-template <class Tag, int DP, int WK, bool VEC>
+template <class Tag, int DP, int WK, bool VEC, bool PLAIN>
 __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   using T = Tile<Tag, DP>;
   using F = FwdShape<Tag, DP, WK>;
-  using Direct = DirectStates<Tag, DP, F::BN>;
+  using Direct = DirectStates<Tag, DP, F::BN, PLAIN, false>;
   constexpr int NB = F::NB, DT = T::DT;
   extern __shared__ __align__(512) char attn_smem[];
   char *const smem = attn_smem;
@@ -605,7 +612,7 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_kernel(AttnArgs a) {
   u32x4 qf[T::NU];
   load_rows<Tag, DP, VEC>(a, a.q, b, hk, r, lane, qf);
   const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
-  const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
+  const uint8_t *mask = !PLAIN && a.mask ? a.mask + b * a.mask_b : nullptr;
   StateMover<Tag, DP, VEC, F::BN, 256> mk, mv;
   uint32_t sight = 1;
   const int rowlane = T::rowlane(lane), collane = T::collane(lane);
@@ -958,32 +965,53 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 // off afterwards.
 template <class Tag> constexpr bool kStart = Tag::W16;
 constexpr float kBlind = -INFINITY;  // start of a row that sees nothing; float32: its negative
-// Kept for the kernel of dk and dv by one lane a row (`keep`).
-template <class Tag, int DP, bool VEC>
-__device__ inline float2 row_stat(const AttnArgs &a, int64_t b, int hk, int r, int lane, const u32x4 *gf, bool keep) {
-  using T = Tile<Tag, DP>;
-  u32x4 of[T::NU];
-  load_rows<Tag, DP, VEC>(a, a.o, b, hk, r, lane, of);
+template <class Tag> __device__ inline float2 blind_stat() { return make_float2(kStart<Tag> ? kBlind : -kBlind, 0.f); }
+
+template <class Tag> __device__ inline float chunk_dot(u32x4 x, u32x4 y) {
   float d = 0.f;
 #pragma unroll
-  for (int u = 0; u < T::NU; ++u)
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const uint32_t x = of[u][j], y = gf[u][j];
-      if constexpr (Tag::W16)
-        d += to_f32<Tag>((u16)(x & 0xffff)) * to_f32<Tag>((u16)(y & 0xffff)) +
-             to_f32<Tag>((u16)(x >> 16)) * to_f32<Tag>((u16)(y >> 16));
-      else
-        d += __uint_as_float(x) * __uint_as_float(y);
-    }
-  d = other_half_sum(d);
-  float2 st = make_float2(kStart<Tag> ? kBlind : -kBlind, 0.f);
-  if (r < a.R) {
-    const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
-    const float lse = a.lse[(b * a.Hq + hq) * a.Sq + sq];
-    if (lse != -INFINITY) st = kStart<Tag> ? make_float2(-lse / a.scale, -d) : make_float2(lse * kLog2e, d);
-    if (keep && lane < 32) a.rowstat[(b * a.Hk + hk) * a.R + r] = st;
+  for (int j = 0; j < 4; ++j) {
+    if constexpr (Tag::W16)
+      d += to_f32<Tag>((u16)(x[j] & 0xffff)) * to_f32<Tag>((u16)(y[j] & 0xffff)) +
+           to_f32<Tag>((u16)(x[j] >> 16)) * to_f32<Tag>((u16)(y[j] >> 16));
+    else
+      d += __uint_as_float(x[j]) * __uint_as_float(y[j]);
   }
+  return d;
+}
+
+// Statistics of row r of a group, whose do.o is d.
+template <class Tag> __device__ inline float2 stat_of(const AttnArgs &a, int64_t b, int hk, int r, float d) {
+  const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
+  const float lse = a.lse[(b * a.Hq + hq) * a.Sq + sq];
+  if (lse == -INFINITY) return blind_stat<Tag>();
+  return kStart<Tag> ? make_float2(-lse / a.scale, -d) : make_float2(lse * kLog2e, d);
+}
+
+// Those of all rows, ahead of the gradients: 16 lanes a row.  (Taken by the
+// owners of dq before, which the owners of dk and dv then had to wait for; see
+// attn_grads_kernel.)
+template <class Tag, bool VEC>
+__global__ __launch_bounds__(256) void attn_stat_kernel(AttnArgs a) {
+  constexpr int CE = 16 / Tag::ES;
+  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const int lane = threadIdx.x & 15;
+  if (row >= a.B * a.Hk * (int64_t)a.R) return;
+  const int64_t bh = row / a.R, b = bh / a.Hk;
+  const int r = (int)(row - bh * a.R), hk = (int)(bh - b * a.Hk);
+  const char *o = group_row(a, a.o, b, hk, r), *g = group_row(a, a.dout, b, hk, r);
+  float d = 0.f;
+  for (int c = lane; c * CE < a.D; c += 16)
+    d += chunk_dot<Tag>(load_chunk<Tag, VEC>(o, c * CE, a.D), load_chunk<Tag, VEC>(g, c * CE, a.D));
+#pragma unroll
+  for (int m = 8; m > 0; m /= 2) d += __shfl_xor(d, m, 16);
+  if (lane == 0) a.rowstat[row] = stat_of<Tag>(a, b, hk, r, d);
+}
+
+// The lane's row of what attn_stat_kernel left.
+template <class Tag> __device__ inline float2 load_stat(const AttnArgs &a, int64_t bh, int r) {
+  float2 st = blind_stat<Tag>();
+  if (r < a.R) st = a.rowstat[bh * a.R + r];
   return st;
 }
 
@@ -1021,18 +1049,16 @@ __device__ inline void to_ds(f32x16 *s, const f32x16 &dp, float c, float2 st, ui
 // states, WK waves sharing rows and splitting each tile.  Measured, bfloat16,
 // 8 x 32 heads of 512 queries over 3136 states of 128 components: 285 us for
 // three products, 1.1 PFLOP/s.
-template <class Tag, int DP, int WK, bool VEC>
-__global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs a) {
+template <class Tag, int DP, int WK, bool VEC, bool PLAIN>
+__device__ inline void take_dq(const AttnArgs &a, char *smem, int64_t id, int64_t units) {
   using T = Tile<Tag, DP>;
   using F = FwdShape<Tag, DP, WK>;
-  using Direct = DirectStates<Tag, DP, F::BN>;
+  using Direct = DirectStates<Tag, DP, F::BN, PLAIN, !PLAIN>;
   constexpr int DT = T::DT, NB = F::NB;
-  extern __shared__ __align__(512) char attn_smem[];
-  char *const smem = attn_smem;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5;
   const int wr = wave % F::WR, wk = wave / F::WR;
   const int tiles = (a.R + F::BM - 1) / F::BM;
-  const int64_t unit = unit_of(blockIdx.x, gridDim.x), bh = unit / tiles, b = bh / a.Hk;
+  const int64_t unit = unit_of(id, units), bh = unit / tiles, b = bh / a.Hk;
   const int rt = (int)(unit - bh * tiles), hk = (int)(bh - b * a.Hk);
   const int len = length_of(a, b);
   const int t1 = (len + F::BN - 1) / F::BN;
@@ -1040,9 +1066,9 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs
   u32x4 qf[T::NU], gf[T::NU];
   load_rows<Tag, DP, VEC>(a, a.q, b, hk, r, lane, qf);
   load_rows<Tag, DP, VEC>(a, a.dout, b, hk, r, lane, gf);
-  const float2 st = row_stat<Tag, DP, VEC>(a, b, hk, r, lane, gf, wk == 0);
+  const float2 st = load_stat<Tag>(a, bh, r);
   const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
-  const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
+  const uint8_t *mask = !PLAIN && a.mask ? a.mask + b * a.mask_b : nullptr;
   StateMover<Tag, DP, VEC, F::BN, 256> mk, mv;
   uint32_t sight = 1;
   const int rowlane = T::rowlane(lane), collane = T::collane(lane);
@@ -1166,16 +1192,14 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dq_kernel(AttnArgs
 // dq, few rows: as attn_few_kernel.  A block's keys are written to this wave's
 // piece of LDS from the fragments of the first product.
 template <class Tag, int DP, bool VEC>
-__global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_few_dq_kernel(AttnArgs a) {
+__device__ inline void take_few_dq(const AttnArgs &a, char *smem, int64_t id, int64_t units) {
   using T = Tile<Tag, DP>;
   using F = FewShape<Tag, DP>;
   constexpr int DT = T::DT;
-  extern __shared__ __align__(512) char attn_smem[];
-  char *const smem = attn_smem;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5, l31 = lane & 31;
   const int tiles = (a.R + 31) / 32;
-  int64_t unit = unit_of(blockIdx.x, gridDim.x);
+  int64_t unit = unit_of(id, units);
   const int rt = (int)(unit % tiles);
   unit /= tiles;
   const int split = (int)(unit % a.splits);
@@ -1192,7 +1216,7 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_few_dq_kernel(Attn
   const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
   load_rows<Tag, DP, VEC>(a, a.q, b, hk, rt * 32 + l31, lane, qf);
   load_rows<Tag, DP, VEC>(a, a.dout, b, hk, rt * 32 + l31, lane, gf);
-  const float2 st = row_stat<Tag, DP, VEC>(a, b, hk, rt * 32 + l31, lane, gf, split == 0 && wave == 0);
+  const float2 st = load_stat<Tag>(a, bh, rt * 32 + l31);
   const int kt = wave * F::TILE;
   uint32_t sight = 1;
   const int rowlane = T::rowlane(lane), collane = T::collane(lane);
@@ -1294,7 +1318,7 @@ struct RowWalk {
     }
   }
   // To registers, or (DIRECT) to the tiles of LDS at `lds`.
-  template <bool DIRECT>
+  template <bool DIRECT, bool PLAIN>
   __device__ void load(const AttnArgs &a, const char *qb, const char *gb, int tid, M *mq, M *mg, uint32_t lds, int wave) {
     const int d0 = M::chunk(tid) * M::T::CE, dc = VEC ? (d0 < a.D ? d0 : 0) * Tag::ES : 0;
 #pragma unroll
@@ -1306,7 +1330,7 @@ struct RowWalk {
       if constexpr (DIRECT) {
         const int c = M::T::chunk_at(M::chunk(tid), M::row(tid, p)) << 4;
         const uint32_t to = lds + p * 4096 + wave * 1024;
-        if ((ROWS % M::RPP == 0 || wave * (M::RPP / 4) < ROWS) && DirectTile<Tag, DP, ROWS>::has(tid, p, a.D)) {
+        if ((ROWS % M::RPP == 0 || wave * (M::RPP / 4) < ROWS) && DirectTile<Tag, DP, ROWS, PLAIN>::has(tid, p, a.D)) {
           lds_load16(to, q + c);
           lds_load16(to + ROWS * M::T::PITCH, o + c);
         }
@@ -1327,17 +1351,15 @@ struct RowWalk {
   }
 };
 
-template <class Tag, int DP, bool VEC>
-__global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArgs a) {
+template <class Tag, int DP, bool VEC, bool PLAIN>
+__device__ inline void take_dkv(const AttnArgs &a, char *smem, int64_t id, int64_t units) {
   using T = Tile<Tag, DP>;
   using F = DkvShape<Tag, DP>;
   constexpr int DT = T::DT;
-  extern __shared__ __align__(512) char attn_smem[];
-  char *const smem = attn_smem;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5, l31 = lane & 31;
   const int tiles = (a.Sk + 127) / 128;
-  int64_t unit = unit_of(blockIdx.x, gridDim.x);
+  int64_t unit = unit_of(id, units);
   const int kt0 = (int)(unit % tiles);
   unit /= tiles;
   const int part = (int)(unit % a.row_parts);
@@ -1350,7 +1372,7 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
   int t1 = (int)((int64_t)all * (part + 1) / a.row_parts);
   if (kt0 * 128 >= len) t1 = t0;  // no state of the tile is visible
 
-  const bool see = j < len && (!a.mask || a.mask[b * a.mask_b + j * a.mask_s]);
+  const bool see = j < len && (PLAIN || !a.mask || a.mask[b * a.mask_b + j * a.mask_s]);
   u32x4 kf[T::NU], vf[T::NU];
   const int rowlane = T::rowlane(lane), collane = T::collane(lane);
   const int val = F::VAL + wave * 32 * T::PITCH + rowlane;  // this wave's values
@@ -1365,17 +1387,13 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
   RowWalk<Tag, DP, VEC, F::BR> walk;
   const char *qb = a.q.p + b * a.q.b + (int64_t)hk * a.G * a.q.h, *gb = a.dout.p + b * a.dout.b + (int64_t)hk * a.G * a.dout.h;
   walk.start(a, t0 * F::BR, tid);
-  const float2 blind = make_float2(kStart<Tag> ? kBlind : -kBlind, 0.f);
-  float2 st = blind;
+  float2 st;
   auto load = [&](int t) {
-    walk.template load<VEC>(a, qb, gb, tid, &mq, &mg, lds_offset(smem) + (t & 1) * 2 * F::TILE, wave);
-    if (tid < F::BR) {
-      st = blind;
-      if (t * F::BR + tid < a.R) st = a.rowstat[bh * a.R + t * F::BR + tid];
-    }
+    walk.template load<VEC, PLAIN>(a, qb, gb, tid, &mq, &mg, lds_offset(smem) + (t & 1) * 2 * F::TILE, wave);
+    if (tid < F::BR) st = load_stat<Tag>(a, bh, t * F::BR + tid);
   };
   f32x16 dk[DT] = {}, dv[DT] = {};
-  if constexpr (VEC) DirectTile<Tag, DP, F::BR>::clear(smem, 4, a.D, tid);
+  if constexpr (VEC) DirectTile<Tag, DP, F::BR, PLAIN>::clear(smem, 4, a.D, tid);
   if (t0 < t1) load(t0);
   arrived(kf);
   if constexpr (!F::VLDS) arrived(vf);
@@ -1491,6 +1509,32 @@ __global__ __launch_bounds__(256, Tag::W16 ? 2 : 1) void attn_dkv_kernel(AttnArg
   store_rows<Tag, DP, VEC>(smem + wave * F::OUT, dv, 1.f, a.D, lane, [&](int n) { return row(a.dv, n); });
 }
 
+// dq and dk, dv in one launch: the owners of states take the first `n_dkv`
+// workgroups or (dq_first) the last, the longer ones ahead, so that the chip is
+// filled by the one kind where the other leaves off.  WK: waves that share the
+// rows of dq, 0 for few rows.  PLAIN: whole rows without a mask, which needs
+// fewer registers.  As many waves a SIMD as the owners of states can have on
+// their own.  Measured against kernels one after the other (the first taking
+// the rows' statistics on its way), bfloat16: 2 x 8 heads of 200 queries over
+// 1001 states of 64 components 24 -> 19 us; float16, 12 x 6 heads of 333 over
+// 1001 masked states of 72 components 79 -> 56; 8 x 32 heads of 2048 over 6272
+// of 128 components 2685 -> 2652.
+template <class Tag, int DP, int WK, bool VEC, bool PLAIN>
+__global__ __launch_bounds__(256, Tag::W16 ? (DP <= 32 ? 4 : DP <= 64 ? 3 : 2) : DP <= 64 ? 2 : 1) void attn_grads_kernel(AttnArgs a, int n_dq, int n_dkv,
+                                                                                      int dq_first) {
+  extern __shared__ __align__(512) char attn_smem[];
+  const int id = blockIdx.x, at = dq_first ? id - n_dq : id;
+  if (at >= 0 && at < n_dkv) {
+    take_dkv<Tag, DP, VEC, PLAIN>(a, attn_smem, at, n_dkv);
+  } else {
+    const int dq = dq_first ? id : id - n_dkv;
+    if constexpr (WK == 0)
+      take_few_dq<Tag, DP, VEC>(a, attn_smem, dq, n_dq);
+    else
+      take_dq<Tag, DP, WK, VEC, PLAIN>(a, attn_smem, dq, n_dq);
+  }
+}
+
 // All gradients of a handful of rows in one pass over the states (16-bit, at
 // most one_pass_rows a key head: learned queries that read a map): the states,
 // read and written once, bound it.  A workgroup keeps a key head's
@@ -1547,7 +1591,7 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
     Mover<Tag, DP, F::ROWS, 256> mq, mg;
     RowWalk<Tag, DP, VEC, F::ROWS> walk;
     walk.start(a, 0, tid);
-    walk.template load<false>(a, a.q.p + b * a.q.b + (int64_t)hk * a.G * a.q.h,
+    walk.template load<false, false>(a, a.q.p + b * a.q.b + (int64_t)hk * a.G * a.q.h,
                               a.dout.p + b * a.dout.b + (int64_t)hk * a.G * a.dout.h, tid, &mq, &mg, 0, 0);
     mq.cut(a.D, tid);
     mg.cut(a.D, tid);
@@ -1557,7 +1601,13 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
       u32x4 gf[NU];
       const int r = wave * 32 + l31;
       load_rows<Tag, DP, VEC>(a, a.dout, b, hk, r, lane, gf);
-      const float2 st = row_stat<Tag, DP, VEC>(a, b, hk, r, lane, gf, false);
+      u32x4 of[NU];
+      load_rows<Tag, DP, VEC>(a, a.o, b, hk, r, lane, of);
+      float d = 0.f;
+#pragma unroll
+      for (int u = 0; u < NU; ++u) d += chunk_dot<Tag>(of[u], gf[u]);
+      d = other_half_sum(d);
+      const float2 st = r < a.R ? stat_of<Tag>(a, b, hk, r, d) : blind_stat<Tag>();
       if (h == 0) {
         ((float *)(smem + F::STAT))[r] = st.x;
         ((float *)(smem + F::STAT))[F::ROWS + r] = st.y;
@@ -1722,11 +1772,24 @@ hipError_t launch_fwd(const AttnArgs &a, hipStream_t stream) {
     WBMM_ATTN_LAUNCH((attn_few_kernel<Tag, DP, VEC>), bh * ((a.R + 31) / 32) * a.splits, (FewShape<Tag, DP>::lds(a.R)), a);
     if (a.splits > 1) WBMM_ATTN_LAUNCH((attn_join_kernel<Tag>), (bh * a.R * a.D + 255) / 256, 0, a);
   } else if (a.tile_rows == 64) {
-    WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 2, VEC>), bh * ((a.R + 63) / 64), (FwdShape<Tag, DP, 2>::LDS), a);
+    WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 2, VEC, false>), bh * ((a.R + 63) / 64), (FwdShape<Tag, DP, 2>::LDS), a);
+  } else if (VEC && a.D == DP && !a.mask) {
+    WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 1, VEC, VEC>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
   } else {
-    WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 1, VEC>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
+    WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 1, VEC, false>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
   }
   return hipSuccess;
+}
+
+template <class Tag, int DP, int WK, bool VEC, bool PLAIN>
+void launch_grads(const AttnArgs &a, int dq_lds, hipStream_t stream) {
+  const int64_t bh = a.B * a.Hk, tile = a.tile_rows;
+  const int n_dq = (int)(bh * ((a.R + tile - 1) / tile) * a.splits);
+  const int n_dkv = (int)(bh * ((a.Sk + 127) / 128) * a.row_parts), dkv_lds = DkvShape<Tag, DP>::LDS;
+  // (three products of a tile with all states, four with all rows)
+  const bool dq_first = 3 * tile * (a.Sk / a.splits) > 4 * 128 * (int64_t)(a.R / a.row_parts);
+  attn_grads_kernel<Tag, DP, WK, VEC, PLAIN>
+      <<<dim3((unsigned)(n_dq + n_dkv)), dim3(256), dq_lds > dkv_lds ? dq_lds : dkv_lds, stream>>>(a, n_dq, n_dkv, dq_first);
 }
 
 template <class Tag, int DP, bool VEC>
@@ -1749,24 +1812,23 @@ hipError_t launch_bwd(const AttnArgs &a, hipStream_t stream) {
       return hipSuccess;
     }
   }
-  if (a.R > 0) {
-    if (a.tile_rows == 32) {
-      WBMM_ATTN_LAUNCH((attn_few_dq_kernel<Tag, DP, VEC>), bh * ((a.R + 31) / 32) * a.splits,
-                       (FewShape<Tag, DP>::lds(a.R)), a);
-      if (a.splits > 1) {
-        const SumArgs s = {{a.part_o}, {a.dq}, bh * a.R, a.splits, a.R, a.G, a.Hk, a.D};
-        WBMM_ATTN_LAUNCH((attn_sum_kernel<Tag>), (bh * a.R * a.D + 255) / 256, 0, s);
-      }
-    } else if (a.tile_rows == 64) {
-      WBMM_ATTN_LAUNCH((attn_dq_kernel<Tag, DP, 2, VEC>), bh * ((a.R + 63) / 64), (FwdShape<Tag, DP, 2>::LDS), a);
-    } else {
-      WBMM_ATTN_LAUNCH((attn_dq_kernel<Tag, DP, 1, VEC>), bh * ((a.R + 127) / 128), (FwdShape<Tag, DP, 1>::LDS), a);
-    }
+  const int64_t rows = bh * a.R;
+  if (rows > 0) WBMM_ATTN_LAUNCH((attn_stat_kernel<Tag, VEC>), (rows + 15) / 16, 0, a);
+  if (a.tile_rows == 32)
+    launch_grads<Tag, DP, 0, VEC, false>(a, FewShape<Tag, DP>::lds(a.R), stream);
+  else if (a.tile_rows == 64)
+    launch_grads<Tag, DP, 2, VEC, false>(a, FwdShape<Tag, DP, 2>::LDS, stream);
+  else if (VEC && a.D == DP && !a.mask)
+    launch_grads<Tag, DP, 1, VEC, VEC>(a, FwdShape<Tag, DP, 1>::LDS, stream);
+  else
+    launch_grads<Tag, DP, 1, VEC, false>(a, FwdShape<Tag, DP, 1>::LDS, stream);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  if (a.splits > 1) {
+    const SumArgs s = {{a.part_o}, {a.dq}, rows, a.splits, a.R, a.G, a.Hk, a.D};
+    WBMM_ATTN_LAUNCH((attn_sum_kernel<Tag>), (rows * a.D + 255) / 256, 0, s);
   }
-  if (a.Sk == 0) return hipSuccess;
-  const int64_t n_dkv = bh * ((a.Sk + 127) / 128) * a.row_parts;
-  WBMM_ATTN_LAUNCH((attn_dkv_kernel<Tag, DP, VEC>), n_dkv, (DkvShape<Tag, DP>::LDS), a);
-  if (a.row_parts > 1) {
+  if (a.row_parts > 1 && a.Sk > 0) {
     const SumArgs s = {{a.part_dk, a.part_dv}, {a.dk, a.dv}, bh * a.Sk, a.row_parts, a.Sk, 1, a.Hk, a.D};
     const int64_t n = (bh * a.Sk * a.D + 255) / 256;
     attn_sum_kernel<Tag><<<dim3((unsigned)n, 2), dim3(256), 0, stream>>>(s);

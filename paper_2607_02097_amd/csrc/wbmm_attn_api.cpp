@@ -193,12 +193,12 @@ Space forward_space(const AttnArgs &a) {
 }
 Space backward_space(const AttnArgs &a) {
   Space w = {};
-  // dq's partial sums are spent before those of dk and dv are written
-  w.part_o = w.part_dk = a.one_pass ? 0 : up16(a.B * a.Hk * (int64_t)a.R * 8);
+  w.part_o = a.one_pass ? 0 : up16(a.B * a.Hk * (int64_t)a.R * 8);
   const int64_t dq = a.splits > 1 ? up16((int64_t)a.splits * a.B * a.Hk * a.R * a.D * 4) : 0;
   const int64_t part = a.row_parts > 1 ? up16((int64_t)a.row_parts * a.B * a.Hk * a.Sk * a.D * 4) : 0;
+  w.part_dk = w.part_o + dq;
   w.part_dv = w.part_dk + part;
-  w.total = w.part_o + (dq > 2 * part ? dq : 2 * part);
+  w.total = w.part_dv + part;
   return w;
 }
 
@@ -411,10 +411,11 @@ bool attn_grids_fit(const AttnArgs &a, bool back) {
   constexpr int64_t most = 1 << 23;  // workgroups of 256 threads in a launch
   const int64_t bh = a.B * a.Hk, rows = bh * a.R;
   // (bh is at most 2^30, the tiles of a head fewer: no overflow)
-  if (bh * cdiv(a.R, a.one_pass ? 1 << 30 : a.tile_rows) * a.splits > most) return false;
+  const int64_t of_rows = bh * cdiv(a.R, a.one_pass ? 1 << 30 : a.tile_rows) * a.splits;
+  if (of_rows > most) return false;
   if (a.splits > 1 && rows > most * 256 / a.D) return false;
   if (!back) return true;
-  if (!a.one_pass && bh * cdiv(a.Sk, 128) > most / a.row_parts) return false;
+  if (!a.one_pass && (rows > most * 16 || bh * cdiv(a.Sk, 128) * a.row_parts > most - of_rows)) return false;
   return a.row_parts == 1 || bh * a.Sk <= most * 256 / a.D;
 }
 
