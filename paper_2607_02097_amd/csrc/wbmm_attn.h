@@ -906,46 +906,70 @@ __global__ __launch_bounds__(256, Tag::W16 || DP <= 64 ? 2 : 1) void attn_few_ke
   }
 }
 
+// Components of a row that a thread of the joining kernels takes (a thread a
+// component, with its position from 64-bit divisions, spent 20 us on 25 MB).
+template <bool VEC> constexpr int kJoin = VEC ? 4 : 1;
+template <bool VEC> __device__ inline void load_part(const float *p, float *v) {
+  if constexpr (VEC) {
+    const f32x4 x = *(const f32x4 *)p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = x[i];
+  } else {
+    v[0] = *p;
+  }
+}
+template <class Tag, bool VEC> __device__ inline void store_part(char *row, int d, const float *v) {
+  if constexpr (!VEC)
+    store1<Tag>(row, d, v[0]);
+  else if constexpr (Tag::W16)
+    *(u32x2 *)(row + d * 2) = (u32x2){pack2<Tag>(v[0], v[1]), pack2<Tag>(v[2], v[3])};
+  else
+    *(f32x4 *)(row + d * 4) = (f32x4){v[0], v[1], v[2], v[3]};
+}
+
 // Joins the partial results of the splits, weighted by their shares of the
-// sum, in their order.  A thread takes one component of one row; the loads of
-// eight splits leave together.
-template <class Tag>
+// sum, in their order.  The loads of eight splits leave together.
+template <class Tag, bool VEC>
 __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
-  const int64_t n = a.B * a.Hk * (int64_t)a.R;
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (e >= n * a.D) return;
-  const int64_t row = e / a.D;
-  const int d = (int)(e - row * a.D);
-  float top = -INFINITY, sum = 0.f, o = 0.f;
+  constexpr int V = kJoin<VEC>;
+  const uint32_t n = (uint32_t)a.B * a.Hk * a.R, e = blockIdx.x * 256 + threadIdx.x;  // (n D is at most 2^31)
+  const uint32_t per = (uint32_t)a.D / V, row = e / per;
+  if (row >= n) return;
+  const int d = (int)(e - row * per) * V;
+  float top = -INFINITY, sum = 0.f, o[V] = {};
   for (int s0 = 0; s0 < a.splits; s0 += 8) {
-    float l[8], p[8];
+    float l[8], p[8][V];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const int s = s0 + i < a.splits ? s0 + i : a.splits - 1;
-      l[i] = a.part_l[s * n + row];
-      p[i] = a.part_o[(s * n + row) * a.D + d];
+      const int64_t at = (int64_t)s * n + row;
+      l[i] = a.part_l[at];
+      load_part<VEC>(a.part_o + at * a.D + d, p[i]);
     }
     float t = top;
 #pragma unroll
     for (int i = 0; i < 8; ++i) t = fmaxf(t, l[i]);
     const float sub = t == -INFINITY ? 0.f : t, fix = exp2_(top - sub);
     sum *= fix;
-    o *= fix;
+#pragma unroll
+    for (int k = 0; k < V; ++k) o[k] *= fix;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const float w = s0 + i < a.splits ? exp2_(l[i] - sub) : 0.f;
       sum += w;
-      o += w * p[i];
+#pragma unroll
+      for (int k = 0; k < V; ++k) o[k] += w * p[i][k];
     }
     top = t;
   }
-  o = sum == 0.f ? 0.f : o / sum;
-  const int64_t bh = row / a.R, b = bh / a.Hk;
+#pragma unroll
+  for (int k = 0; k < V; ++k) o[k] = sum == 0.f ? 0.f : o[k] / sum;
+  const uint32_t bh = row / (uint32_t)a.R, b = bh / (uint32_t)a.Hk;
   const int r = (int)(row - bh * a.R), hk = (int)(bh - b * a.Hk);
-  store1<Tag>(group_row(a, a.o, b, hk, r), d, o);
+  store_part<Tag, VEC>(group_row(a, a.o, b, hk, r), d, o);
   const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
   if (a.lse && d == 0)
-    a.lse[(b * a.Hq + hq) * a.Sq + sq] = (sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum)) * kLn2;
+    a.lse[((int64_t)b * a.Hq + hq) * a.Sq + sq] = (sum == 0.f ? -INFINITY : top + __builtin_amdgcn_logf(sum)) * kLn2;
 }
 
 // ----------------------------------------------------------------- backward
@@ -1735,25 +1759,33 @@ struct SumArgs {
   int parts, N, G, Hk, D;
 };
 
-template <class Tag>
+template <class Tag, bool VEC>
 __global__ __launch_bounds__(256) void attn_sum_kernel(SumArgs a) {
-  const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, n = a.rows * a.D;
-  if (e >= n) return;
-  const float *part = a.part[blockIdx.y];
+  constexpr int V = kJoin<VEC>;
+  const uint32_t e = blockIdx.x * 256 + threadIdx.x, per = (uint32_t)a.D / V, row = e / per;  // (rows D is at most 2^31)
+  if (row >= (uint32_t)a.rows) return;
+  const int d = (int)(e - row * per) * V;
+  const float *part = a.part[blockIdx.y] + (int64_t)row * a.D + d;
   const Tokens &t = a.out[blockIdx.y];
-  float sum = 0.f;
+  const int64_t step = a.rows * a.D;
+  float sum[V] = {};
   for (int p0 = 0; p0 < a.parts; p0 += 8) {
-    float v[8];
+    float v[8][V] = {};
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = p0 + i < a.parts ? part[(p0 + i) * n + e] : 0.f;
+    for (int i = 0; i < 8; ++i)
+      if (p0 + i < a.parts) load_part<VEC>(part + (p0 + i) * step, v[i]);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum += v[i];
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int k = 0; k < V; ++k) sum[k] += v[i][k];
   }
-  const int64_t row = e / a.D, bh = row / a.N, b = bh / a.Hk;
-  const int d = (int)(e - row * a.D), r = (int)(row - bh * a.N), hk = (int)(bh - b * a.Hk);
-  const int s = r / a.G, g = r - s * a.G;
-  store1<Tag>(t.p + b * t.b + s * t.s + (int64_t)(hk * a.G + g) * t.h, d, sum);
+  const uint32_t bh = row / (uint32_t)a.N, b = bh / (uint32_t)a.Hk;
+  const int r = (int)(row - bh * a.N), hk = (int)(bh - b * a.Hk), s = r / a.G, g = r - s * a.G;
+  store_part<Tag, VEC>(t.p + (int64_t)b * t.b + s * t.s + (int64_t)(hk * a.G + g) * t.h, d, sum);
 }
+
+// Workgroups that join rows of D components.
+template <bool VEC> int64_t joiners(int64_t rows, int D) { return (rows * (D / kJoin<VEC>) + 255) / 256; }
 
 // ---------------------------------------------------------------- launchers
 
@@ -1770,7 +1802,7 @@ hipError_t launch_fwd(const AttnArgs &a, hipStream_t stream) {
   const int64_t bh = a.B * a.Hk;
   if (a.tile_rows == 32) {
     WBMM_ATTN_LAUNCH((attn_few_kernel<Tag, DP, VEC>), bh * ((a.R + 31) / 32) * a.splits, (FewShape<Tag, DP>::lds(a.R)), a);
-    if (a.splits > 1) WBMM_ATTN_LAUNCH((attn_join_kernel<Tag>), (bh * a.R * a.D + 255) / 256, 0, a);
+    if (a.splits > 1) WBMM_ATTN_LAUNCH((attn_join_kernel<Tag, VEC>), joiners<VEC>(bh * a.R, a.D), 0, a);
   } else if (a.tile_rows == 64) {
     WBMM_ATTN_LAUNCH((attn_fwd_kernel<Tag, DP, 2, VEC, false>), bh * ((a.R + 63) / 64), (FwdShape<Tag, DP, 2>::LDS), a);
   } else if (VEC && a.D == DP && !a.mask) {
@@ -1807,7 +1839,7 @@ hipError_t launch_bwd(const AttnArgs &a, hipStream_t stream) {
       if (!half) WBMM_ATTN_LAUNCH((attn_rows_bwd_kernel<Tag, DP, NRB, VEC>), bh * a.splits, (RowsShape<Tag, DP, NRB>::LDS), a);
       if (a.splits > 1) {
         const SumArgs s = {{a.part_o}, {a.dq}, bh * a.R, a.splits, a.R, a.G, a.Hk, a.D};
-        WBMM_ATTN_LAUNCH((attn_sum_kernel<Tag>), (bh * a.R * a.D + 255) / 256, 0, s);
+        WBMM_ATTN_LAUNCH((attn_sum_kernel<Tag, VEC>), joiners<VEC>(bh * a.R, a.D), 0, s);
       }
       return hipSuccess;
     }
@@ -1826,12 +1858,11 @@ hipError_t launch_bwd(const AttnArgs &a, hipStream_t stream) {
   if (e != hipSuccess) return e;
   if (a.splits > 1) {
     const SumArgs s = {{a.part_o}, {a.dq}, rows, a.splits, a.R, a.G, a.Hk, a.D};
-    WBMM_ATTN_LAUNCH((attn_sum_kernel<Tag>), (rows * a.D + 255) / 256, 0, s);
+    WBMM_ATTN_LAUNCH((attn_sum_kernel<Tag, VEC>), joiners<VEC>(rows, a.D), 0, s);
   }
   if (a.row_parts > 1 && a.Sk > 0) {
     const SumArgs s = {{a.part_dk, a.part_dv}, {a.dk, a.dv}, bh * a.Sk, a.row_parts, a.Sk, 1, a.Hk, a.D};
-    const int64_t n = (bh * a.Sk * a.D + 255) / 256;
-    attn_sum_kernel<Tag><<<dim3((unsigned)n, 2), dim3(256), 0, stream>>>(s);
+    attn_sum_kernel<Tag, VEC><<<dim3((unsigned)joiners<VEC>(bh * a.Sk, a.D), 2), dim3(256), 0, stream>>>(s);
     return hipGetLastError();
   }
   return hipSuccess;
