@@ -351,12 +351,9 @@ constexpr int64_t kUnits = 256;  // compute units
 int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 int64_t clamp(int64_t n, int64_t lo, int64_t hi) { return n < lo ? lo : n > hi ? hi : n; }
 
-// Larger tiles of rows read the states less often and feed the matrix cores
-// better, but need a workgroup for three compute units in four: measured,
-// bfloat16, 128 / 64 / 32 rows: 192 heads of 100 rows 18.5 / 19.7 / 23.5 us
-// (192 workgroups of 128 rows), 32 heads of 512 rows 24 / 20 / 27 us (128), 16
-// heads of 512 rows over 3136 states 56 / 43 / 23 us (64).
-// Tiles of 32 rows can take the states in parts, for a workgroup on every
+// By the number of workgroups.  Larger tiles of rows read the states less often
+// and feed the matrix cores better, but need one for three compute units in
+// four.  Tiles of 32 rows can take the states in parts, for a workgroup on every
 // compute unit (one unit reads about 50 GB/s, whatever its waves), of 96 states
 // at least, since the parts are joined by a launch of its own; single tokens
 // over long sequences in up to eight workgroups a unit, so that unequal lengths
@@ -364,7 +361,7 @@ int64_t clamp(int64_t n, int64_t lo, int64_t hi) { return n < lo ? lo : n > hi ?
 // part, 8.1 in two; 784 states 11.7 us in one part, 9.1 in four, 8.2 in eight;
 // 12544 states 129 us in one, 25 in 8, 17 in 24 to 32.  32 tokens over 12544
 // states each: 294 us in one part, 285 in eight, 306 in 32.
-void plan_rows(AttnArgs *a) {
+void plan_by_count(AttnArgs *a) {
   const int64_t bh = a->B * a->Hk, enough = kUnits * 3 / 4;
   a->splits = 1;
   if (a->R > 64 && bh * cdiv(a->R, 128) >= enough) {
@@ -380,31 +377,84 @@ void plan_rows(AttnArgs *a) {
   }
 }
 
-}  // namespace
+// An account of a launch's time.  Workgroups that own rows, and for gradients
+// others that own states, run through products of 32 x 32 blocks, one wave's
+// after the other; the launch takes the root of the sum of the squares of the
+// longest of them and of all of them spread over the chip.  Larger tiles of rows
+// read the states less often.  Parts take a launch more, and their sums are
+// written and read.
+struct Account {
+  int products;          // of a block, for owners of rows
+  double start;          // of a workgroup, in products
+  double few;            // a block in tiles of 32 rows, whose states come from memory
+  double spread[3];      // what shares a unit, in tiles of 128, 64 and 32 rows
+  double block, launch;  // us
+};
+constexpr double kPartRate = 2.2e6;  // bytes of partial sums, written and read, a us
 
-void attn_plan_forward(Dt, AttnArgs *a) {
-  plan_rows(a);
-  a->row_parts = 1;
+// Tiles and parts that take the least time by an account.
+void plan_by(const Account &c, bool grads, AttnArgs *a) {
+  const double bh = (double)(a->B * a->Hk), states = (double)cdiv(a->Sk, 32), rows = (double)cdiv(a->R, 32);
+  const double n_states = grads ? bh * cdiv(a->Sk, 128) : 0;
+  constexpr int counts[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+  double best = INFINITY;
+  for (int i = 0, tile = 128; i < 3; ++i, tile /= 2) {
+    if (tile > 32 && a->R <= tile / 2) continue;
+    const double n_rows = bh * cdiv(a->R, tile);
+    for (int s : counts) {
+      if (s > 1 && (tile > 32 || s > a->Sk / 96 || n_rows * s > 4 * kUnits)) break;
+      const double by_rows = c.start + c.products * states * tile / 128 / s * (tile == 32 ? c.few : 1);
+      for (int p : counts) {
+        if (p > 1 && (p > a->R / 64 || !grads || n_states * p > 4 * kUnits)) break;
+        const double by_states = grads ? c.start + 3.6 * rows / p : 0, longest = by_rows > by_states ? by_rows : by_states;
+        const double all = (n_rows * s * by_rows * c.spread[i] + n_states * p * by_states * c.spread[0]) / kUnits;
+        double t = c.block * sqrt(longest * longest + all * all);
+        if (s > 1) t += c.launch + bh * a->R * a->D * 8 * s / kPartRate;
+        if (p > 1) t += c.launch + bh * a->Sk * a->D * 16 * p / kPartRate;
+        if (t < best) best = t, a->tile_rows = tile, a->splits = s, a->row_parts = p;
+      }
+    }
+  }
 }
 
-// Few rows (16-bit): all gradients in one pass over the states, whose parts
-// follow the same measure: 64 key heads of 128 components over 3136 states
+}  // namespace
+
+// The constants of the accounts are fitted to 184 (forward) and 200 sizes (4 to
+// 192 heads, 33 to 4000 rows, 48 to 8000 states, 32 to 128 components), each in up
+// to 30 arrangements.  What they choose takes 3.5 % more than the best of them on
+// average (the gradients 2 %, in float32 5 %), where limits on the numbers of
+// workgroups took 6 % (13 %, 10 %); in float32 the forward, at 5 % by either, goes
+// by the limits.  bfloat16, forward: 16 heads of 590 rows over 51 states in tiles
+// of 128 rows, not 32: 12.2 -> 6.6 us.  Gradients: 16 heads of 600 rows, 784
+// states of 128 components: 128 rows a tile, no parts, 32 us (in tiles of 64 rows
+// 35, of 32 rows 40, rows in two parts 46); 8 heads of 800 rows, 196 states: rows
+// in 6 parts, 23 us (one part 37).
+void attn_plan_forward(Dt dt, AttnArgs *a) {
+  const int wide = (a->D + 31) / 32 * 32;  // components, as they are multiplied
+  a->row_parts = 1;
+  if (a->R <= 32 || dt == Dt::F32)
+    plan_by_count(a);
+  else
+    plan_by({2, 8.5, 1.2, {0.96, 1.63, 1.84}, 4.75e-3 * (wide + 64), 2.5}, false, a);
+}
+
+// Few rows (16-bit): all gradients in one pass over the states, in parts for a
+// workgroup on every unit: 64 key heads of 128 components over 3136 states
 // 114 us in one part, 49 in four (one workgroup a unit), 60 in eight; 192
 // heads 24 us in one part, 26 in two.
-// Otherwise dk and dv take the rows in parts only where the states' tiles
-// leave most of the chip idle, of at least 512 rows (float32, whose products
-// take sixteen times as long: 128), since the parts are summed by a launch of
-// its own: one key head of 16384 rows and 64 states takes 402 us in one part and
-// 37 in 32, 8 heads of 256 rows and 784 states 40 us in one and 47 in two.
 void attn_plan_backward(Dt dt, AttnArgs *a) {
-  plan_rows(a);
-  const int64_t bh = a->B * a->Hk, wgs = bh * cdiv(a->Sk, 128);
+  const int64_t bh = a->B * a->Hk;
   if (dt != Dt::F32 && a->R > 0 && a->R <= one_pass_rows(a->D) && a->Sk > 0) {
+    a->tile_rows = 32;
     a->one_pass = a->row_parts = 1;
     a->splits = (int)clamp(bh > 0 ? kUnits / bh : 1, 1, clamp(a->Sk / 96, 1, 64));
     return;
   }
-  a->row_parts = (int)clamp(wgs > 0 ? kUnits / wgs : 1, 1, clamp(a->R / (dt == Dt::F32 ? 128 : 512), 1, 64));
+  const int wide = (a->D + 31) / 32 * 32;
+  if (dt == Dt::F32)
+    plan_by({3, 7.4, 0.98, {1.13, 1.37, 1.13}, 50e-3 * (wide + 16), 5}, true, a);
+  else
+    plan_by({3, 16.5, 2, {0.62, 0.92, 1.24}, 5.75e-3 * (wide + 64), 5}, true, a);
 }
 
 bool attn_grids_fit(const AttnArgs &a, bool back) {
