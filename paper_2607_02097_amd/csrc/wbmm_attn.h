@@ -976,9 +976,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 //
 // With p recomputed from the forward's lse, delta_r = do_r.o_r and
 // ds = p (do.v - delta):  dq = scale ds K,  dk = scale ds^T Q,  dv = p^T do.
-// Two kernels recompute the scores, one per owner of the results (rows for
-// dq, states for dk and dv), so every sum has one owner and a fixed order: no
-// atomics, and the same bits every time.
+// The scores are recomputed twice, by the owners of rows for dq and by the
+// owners of states for dk and dv, so every sum has one owner and a fixed order:
+// no atomics, and the same bits every time.
 
 // Statistics of the lane's row.  16-bit: what its products start from,
 // {-lse / scale, -delta}, so that they come out as the weight's exponent and as
@@ -1012,9 +1012,9 @@ template <class Tag> __device__ inline float2 stat_of(const AttnArgs &a, int64_t
   return kStart<Tag> ? make_float2(-lse / a.scale, -d) : make_float2(lse * kLog2e, d);
 }
 
-// Those of all rows, ahead of the gradients: 16 lanes a row.  (Taken by the
-// owners of dq before, which the owners of dk and dv then had to wait for; see
-// attn_grads_kernel.)
+// Those of all rows, ahead of the gradients: 16 lanes a row, bound by memory
+// (131072 rows of 128 components, bfloat16: 15 us, 4.5 TB/s).  Taken by the
+// owners of dq instead, the owners of dk and dv would have to wait for them.
 template <class Tag, bool VEC>
 __global__ __launch_bounds__(256) void attn_stat_kernel(AttnArgs a) {
   constexpr int CE = 16 / Tag::ES;
@@ -1070,9 +1070,9 @@ __device__ inline void to_ds(f32x16 *s, const f32x16 &dp, float c, float2 st, ui
 }
 
 // dq: as the forward, a workgroup takes 32 (4 / WK) rows and runs over all
-// states, WK waves sharing rows and splitting each tile.  Measured, bfloat16,
-// 8 x 32 heads of 512 queries over 3136 states of 128 components: 285 us for
-// three products, 1.1 PFLOP/s.
+// states, WK waves sharing rows and splitting each tile.  Measured on its own,
+// bfloat16, 8 x 32 heads of 512 queries over 3136 states of 128 components:
+// 285 us for three products, 1.1 PFLOP/s.
 template <class Tag, int DP, int WK, bool VEC, bool PLAIN>
 __device__ inline void take_dq(const AttnArgs &a, char *smem, int64_t id, int64_t units) {
   using T = Tile<Tag, DP>;
