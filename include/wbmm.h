@@ -343,7 +343,8 @@ wbmm_status wbmm_rotary_backward(const wbmm_rotary_args *args, void *stream);
  * sums and a float32 softmax; p and its gradient are rounded to the type as
  * operands of the second products (float16: p's gradient has to be in the
  * type's range, as with any loss scale).  float32: float32 products.
- * Sums have a fixed order: results are reproducible bit for bit.
+ * Sums have a fixed order: results are reproducible bit for bit.  States 16 MB
+ * or more apart (stride_s) are moved element by element.
  *
  * workspace: device buffer of at least the size that the matching query
  * returns for the same arguments (0: may be NULL), 16-byte aligned, any

@@ -827,7 +827,7 @@ __global__ __launch_bounds__(256, Tag::W16 || DP <= 64 ? 2 : 1) void attn_few_ke
     for (int u = 0; u < T::NU; ++u) s = mma_chunk<Tag>(kf[u], qf[u], s);
     uint32_t see = 0xffffffffu;
     if (mask || (t + 1) * 32 > len) see = (uint32_t)sight_bits(sight, t * 32, 32, len, lane);
-    mv.hide(mask != nullptr, see, a.D, lane);
+    mv.hide(see != 0xffffffffu, see, a.D, lane);
     mv.store(smem + vt, lane);
     // (the next block's loads leave behind the last use of this one's: where
     // they may or may not have left, a wait would have to take them in)

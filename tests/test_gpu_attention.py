@@ -675,3 +675,36 @@ def test_attention_small_and_large_scales():
         q, k, v, g = attention_inputs(2, 70, 50, 2, 2, 32, dtype, seed=170)
         for scale in (1e-30, 1e-4, 16.0):
             run_and_check(q, k, v, g, dtype, scale=scale, tag="scale %g" % scale)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("kind", ["", "lens", "lens+mask", "gap"])
+@pytest.mark.parametrize("Sq,Sk,Hq,Hk,D", [(130, 700, 1, 1, 64), (100, 330, 2, 1, 128), (70, 500, 3, 1, 37),
+                                           (520, 130, 2, 1, 72)])
+def test_attention_gradients_in_parts(Sq, Sk, Hq, Hk, D, kind, dtype):
+    """Few heads: states and rows both in parts, whose partial sums share a
+    workspace; hidden states, whole tiles of them too, hold NaN."""
+    B = 3
+    q, k, v, g = attention_inputs(B, Sq, Sk, Hq, Hk, D, dtype, seed=180)
+    lens, mask = hidden(B, Sk, kind)
+    if kind == "gap":
+        mask = torch.ones(B, Sk, dtype=torch.bool)
+        mask[0, 30:Sk - 3] = mask[1, :64] = mask[2, 64:128] = False
+    see = torch.ones(B, Sk, dtype=torch.bool) if mask is None else mask.clone()
+    if lens is not None:
+        see &= torch.arange(Sk)[None] < lens[:, None]
+    k[~see], v[~see] = float("nan"), float("nan")
+    _, _, (_, dk, dv) = run_and_check(q, k, v, g, dtype, lens, mask)
+    assert bool((dk.cpu()[~see] == 0).all()) and bool((dv.cpu()[~see] == 0).all())
+
+
+@pytest.mark.parametrize("Sq,D", [(128, 128), (128, 72), (50, 64), (1, 64)])
+def test_attention_infinite_values_keep_their_sign(Sq, D):
+    """An infinite component of a visible state's values comes out as itself,
+    the last state's too, beside which a tile is filled up."""
+    q, k, v, _ = (t.cuda() for t in attention_inputs(25, Sq, 70, 8, 8, D, "bf16", seed=190))
+    clean, _ = W.wbmm_cross_attention_forward(q, k, v)
+    v[:, -1, :, 5] = float("inf")
+    out, _ = W.wbmm_cross_attention_forward(q, k, v)
+    keep = torch.arange(D, device="cuda") != 5
+    assert bool((out[..., 5] == float("inf")).all()) and torch.equal(out[..., keep], clean[..., keep])
