@@ -55,8 +55,8 @@ struct Tile {
   static constexpr int NU = DP / (2 * CE);                        // chunk pairs of a row
   static constexpr int DT = DP / 32;
   // The chunk of a row that belongs at a slot.
-  __device__ static int chunk_at(int slot, int row) { return slot ^ swz(row); }
-  __device__ static int swz(int row) {
+  __host__ __device__ static constexpr int chunk_at(int slot, int row) { return slot ^ swz(row); }
+  __host__ __device__ static constexpr int swz(int row) {
     if constexpr (ES == 2) {
       if constexpr (PITCH == 256) return ((row & 3) << 2) | ((row >> 2) & 3);
       if constexpr (PITCH == 128) return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
@@ -324,8 +324,8 @@ struct Mover {
   static constexpr int RPP = THREADS / T::LPC;  // rows a pass
   static constexpr int NP = (ROWS + RPP - 1) / RPP;
   u32x4 r[NP];
-  __device__ static int chunk(int tid) { return tid % T::LPC; }
-  __device__ static int row(int tid, int p) { return tid / T::LPC + p * RPP; }
+  __host__ __device__ static constexpr int chunk(int tid) { return tid % T::LPC; }
+  __host__ __device__ static constexpr int row(int tid, int p) { return tid / T::LPC + p * RPP; }
   // zeroes chunks past D
   __device__ void cut(int D, int tid) {
     if (D <= (T::LPC - 1) * T::CE && chunk(tid) * T::CE >= D) {
@@ -402,13 +402,16 @@ __device__ inline uint32_t lds_offset(const char *p) {
 }
 
 // Places of a thread in tiles of ROWS rows that four waves load.  PLAIN: D = DP
-// and no mask, known ahead.
+// and no mask, known ahead, so that every place has its piece where the tile's
+// rows are as long as the tensors'.  (96 components lie in rows of 128, whose
+// last chunks have nothing behind them in memory.)
 template <class Tag, int DP, int ROWS, bool PLAIN>
 struct DirectTile {
   using M = Mover<Tag, DP, ROWS, 256>;
-  __device__ static bool has(int tid, int p, int D) {
+  __host__ __device__ static constexpr bool has(int tid, int p, int D) {
+    if (PLAIN && M::T::PITCH == DP * Tag::ES) return true;
     // (the swizzle has a period of 16 rows)
-    return PLAIN || M::T::chunk_at(M::chunk(tid), M::row(tid, M::RPP % 16 == 0 ? 0 : p)) * M::T::CE < D;
+    return M::T::chunk_at(M::chunk(tid), M::row(tid, M::RPP % 16 == 0 ? 0 : p)) * M::T::CE < (PLAIN ? DP : D);
   }
   // Zeroes the places past D of `tiles` tiles.
   __device__ static void clear(char *tile, int tiles, int D, int tid) {
