@@ -958,7 +958,8 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
     for (int k = 0; k < V; ++k) o[k] *= fix;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float w = s0 + i < a.splits ? exp2_(l[i] - sub) : 0.f;
+      if (s0 + i >= a.splits) continue;  // (its loads repeat the last part, which may be infinite)
+      const float w = exp2_(l[i] - sub);
       sum += w;
 #pragma unroll
       for (int k = 0; k < V; ++k) o[k] += w * p[i][k];
