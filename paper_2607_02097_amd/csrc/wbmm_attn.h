@@ -333,6 +333,12 @@ struct Mover {
       for (int p = 0; p < NP; ++p) r[p] = (u32x4){0, 0, 0, 0};
     }
   }
+  // zeroes rows from n on
+  __device__ void cut_rows(int n, int tid) {
+#pragma unroll
+    for (int p = 0; p < NP; ++p)
+      if (row(tid, p) >= n) r[p] = (u32x4){0, 0, 0, 0};
+  }
   __device__ void store(char *tile, int tid) const {
 #pragma unroll
     for (int p = 0; p < NP; ++p) {
@@ -427,7 +433,8 @@ struct DirectTile {
     asm volatile("" : "+v"(tid));
 #pragma unroll
     for (int p = 0; p < M::NP; ++p)
-      if (!((see >> (M::row(tid, p) & 63)) & 1)) *(u32x4 *)(tile + p * 4096 + tid * 16) = (u32x4){0, 0, 0, 0};
+      if ((ROWS % M::RPP == 0 || M::row(tid, p) < ROWS) && !((see >> (M::row(tid, p) & 63)) & 1))
+        *(u32x4 *)(tile + p * 4096 + tid * 16) = (u32x4){0, 0, 0, 0};
   }
 };
 
@@ -1330,7 +1337,10 @@ struct DkvShape {
 
 // Tiles of ROWS rows of a group, one after the other.  The query and head of a
 // thread's rows are carried along, so that only the first tile divides.  Rows
-// from R on repeat the last one: their weights are zero.
+// from R on repeat the last one, with weights of zero.  Their upstream gradients
+// have to be zero too, since the last row's may be infinite: element by element
+// they are loaded as zero; whole pieces are zeroed on their way to LDS (cut_rows)
+// or when they have arrived there (DirectTile::hide).
 template <class Tag, int DP, bool VEC, int ROWS>
 struct RowWalk {
   using M = Mover<Tag, DP, ROWS, 256>;
@@ -1367,7 +1377,7 @@ struct RowWalk {
         mg->r[p] = *(const u32x4 *)o;
       } else {
         mq->r[p] = load_chunk<Tag, VEC>(q, d0, a.D);
-        mg->r[p] = load_chunk<Tag, VEC>(o, d0, a.D);
+        mg->r[p] = load_chunk<Tag, VEC>(o, d0, in ? a.D : 0);
       }
       s[p] += step_s;
       g[p] += step_g;
@@ -1430,6 +1440,8 @@ __device__ inline void take_dkv(const AttnArgs &a, char *smem, int64_t id, int64
     float *stat = (float *)(smem + F::STAT) + (t & 1) * 2 * F::BR;
     if constexpr (VEC) {
       lds_loads_done();
+      if ((t + 1) * F::BR > a.R)
+        DirectTile<Tag, DP, F::BR, PLAIN>::hide(smem + gt, ((uint64_t)1 << (a.R - t * F::BR)) - 1, tid);
     } else {
       mq.cut(a.D, tid);
       mg.cut(a.D, tid);
@@ -1623,6 +1635,7 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
                               a.dout.p + b * a.dout.b + (int64_t)hk * a.G * a.dout.h, tid, &mq, &mg, 0, 0);
     mq.cut(a.D, tid);
     mg.cut(a.D, tid);
+    if constexpr (VEC) mg.cut_rows(a.R, tid);
     mq.store(smem + F::Q, tid);
     mg.store(smem + F::G, tid);
     if (wave < F::NRB) {  // (at most four)
