@@ -341,8 +341,8 @@ wbmm_status wbmm_rotary_backward(const wbmm_rotary_args *args, void *stream);
  * [B,Hq,Sq] contiguous.  1 <= D <= 128; 1e-30 <= scale, finite.  B, Sq and
  * Sk may be 0.  16-bit types: products on the matrix cores with float32
  * sums and a float32 softmax; p and its gradient are rounded to the type as
- * operands of the second products (float16: p's gradient has to be in the
- * type's range, as with any loss scale).  float32: float32 products.
+ * operands of the second products (float16: times powers of two that keep them
+ * within the type's normal numbers).  float32: float32 products.
  * Sums have a fixed order: results are reproducible bit for bit.  States 16 MB
  * or more apart (stride_s) are moved element by element.
  *

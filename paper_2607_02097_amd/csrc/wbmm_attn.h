@@ -993,12 +993,14 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 
 // Statistics of the lane's row.  16-bit: what its products start from,
 // {-lse / scale, -delta}, so that they come out as the weight's exponent and as
-// dp - delta, without an instruction more; a row that sees nothing starts from
+// dp - delta, without an instruction more (float16 weights 2^12 larger, which
+// the first of them takes in: kRaiseBack); a row that sees nothing starts from
 // minus infinity, and its weights come out as zero.  In float32 the sums would
 // round at lse's size instead of the products' own (errors of the gradients
 // 1.3e-6 instead of 0.8e-6), so there it is {lse in log2 units, delta}, taken
 // off afterwards.
 template <class Tag> constexpr bool kStart = Tag::W16;
+template <class Tag> constexpr int kRaiseBack = __is_same(Tag, TagF16) ? 12 : 0;
 constexpr float kBlind = -INFINITY;  // start of a row that sees nothing; float32: its negative
 template <class Tag> __device__ inline float2 blind_stat() { return make_float2(kStart<Tag> ? kBlind : -kBlind, 0.f); }
 
@@ -1020,27 +1022,135 @@ template <class Tag> __device__ inline float2 stat_of(const AttnArgs &a, int64_t
   const int sq = r / a.G, hq = hk * a.G + r - sq * a.G;
   const float lse = a.lse[(b * a.Hq + hq) * a.Sq + sq];
   if (lse == -INFINITY) return blind_stat<Tag>();
-  return kStart<Tag> ? make_float2(-lse / a.scale, -d) : make_float2(lse * kLog2e, d);
+  return kStart<Tag> ? make_float2((kRaiseBack<Tag> * kLn2 - lse) / a.scale, -d) : make_float2(lse * kLog2e, d);
+}
+
+// float16's ds.  It goes with the upstream gradient and with the weights: over
+// thousands of states, or without a loss scale, it lies below the type's normal
+// numbers, and with a large loss scale above its largest (64 rows over 6272
+// states, dout of std 1e-3: dq off by 0.0047 of itself as it is, by 0.00031 as
+// follows, where its last rounding alone makes 0.00021).  So it is multiplied by
+// a power of two on its way to the product, taken from a bound that is known
+// ahead,
+//   |ds_rj| <= |dp_rj| + |delta_r| <= 2 B,  B = sum |do_r| max |v|,
+// with the maxima over what shares a sum: for dq the row's own sum |do_r| and the
+// visible states, for dk the rows and the state's own values.  The largest ds
+// then lies below 2^15, and each keeps 2^-38 B of absolute precision (2^-25, half
+// of the type's smallest step, over the power), where it would need 2^-11 of
+// itself.  Powers: 2^13 over B's own power of two, at most 2^100.
+template <class Tag> constexpr bool kPower = __is_same(Tag, TagF16);
+
+__device__ inline int power_for(float bound) {  // its exponent
+  const int e = (int)(__float_as_uint(bound) >> 23) & 255;  // (255: not finite)
+  return 140 - (e > 40 ? e : 40);
+}
+// 2^e, |e| < 127
+__device__ inline float exponent(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+
+// Sum of the magnitudes of a chunk, and their largest as a 16-bit pattern in
+// either half of the result (patterns of magnitudes are in the numbers' order).
+template <class Tag> __device__ inline float chunk_sum(u32x4 x) {
+  float d = 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    d += __builtin_fabsf(to_f32<Tag>((u16)(x[j] & 0xffff))) + __builtin_fabsf(to_f32<Tag>((u16)(x[j] >> 16)));
+  return d;
+}
+typedef u16 u16x2 __attribute__((ext_vector_type(2)));
+__device__ inline u16x2 chunk_top(u32x4 x, u16x2 top) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, x[j] & 0x7fff7fffu));
+  return top;
+}
+__device__ inline uint32_t top_of(u16x2 top) { return top[0] > top[1] ? top[0] : top[1]; }
+
+// Largest value of the wave, in all lanes.
+template <int CTRL> __device__ inline uint32_t turned_max(uint32_t v) {
+  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xf, 0xf, false);
+  return v > o ? v : o;
+}
+__device__ inline uint32_t wave_max(uint32_t v) {
+  // rotations by 8, 4, 2, 1 within the rows of 16 lanes, then across the rows
+  v = turned_max<0x121>(turned_max<0x122>(turned_max<0x124>(turned_max<0x128>(v))));
+  const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+  v = a[0] > a[1] ? a[0] : a[1];
+  const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+  return b[0] > b[1] ? b[0] : b[1];
+}
+// Largest of p[first .. end), magnitudes, in all lanes; eight loads at a time.
+__device__ inline float wave_top(const float *p, int first, int end, int lane) {
+  float m = 0.f;
+  for (int i = first + lane; i - lane < end; i += 512) {
+    float v[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) v[k] = p[i + 64 * k < end ? i + 64 * k : end - 1];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) m = fmaxf(m, v[k]);
+  }
+  return __uint_as_float(wave_max(__float_as_uint(m)));
+}
+
+// max |v| of the visible ones of 32 states, a wave each, four states at a time
+// (all loads leave together, those of hidden states too); workgroup `id` takes
+// 128 states.
+template <class Tag, bool VEC>
+__device__ inline void take_top_v(const AttnArgs &a, uint32_t id) {
+  constexpr int CE = 16 / Tag::ES;
+  const uint32_t tiles = ((uint32_t)a.Sk + 127) / 128, bh = id / tiles;
+  const int64_t b = bh / (uint32_t)a.Hk;
+  const int lane = threadIdx.x & 63, hk = (int)(bh - (uint32_t)b * a.Hk);
+  const int first = (int)(id - bh * tiles) * 128 + (int)(threadIdx.x >> 6) * 32;
+  if (first >= a.Sk) return;
+  const int len = length_of(a, b);
+  const char *vb = a.v.p + b * a.v.b + hk * a.v.h;
+  u16x2 top = {0, 0};
+  u32x4 v[8];
+  uint32_t see[8];
+#pragma unroll
+  for (int p = 0; p < 8; ++p) {
+    const int n = first + 4 * p + (lane >> 4), j = n < a.Sk ? n : a.Sk - 1;
+    v[p] = load_chunk<Tag, VEC>(vb + j * a.v.s, (lane & 15) * CE, a.D);
+    see[p] = a.mask ? a.mask[b * a.mask_b + j * a.mask_s] : 1;
+    if (j >= len) see[p] = 0;
+  }
+#pragma unroll
+  for (int p = 0; p < 8; ++p) top = see[p] ? chunk_top(v[p], top) : top;
+  const uint32_t all = wave_max(top_of(top));
+  if (lane == 0) a.top_v[(int64_t)bh * ((a.Sk + 31) / 32) + first / 32] = to_f32<Tag>((u16)all);
 }
 
 // Those of all rows, ahead of the gradients: 16 lanes a row, bound by memory
 // (131072 rows of 128 components, bfloat16: 15 us, 4.5 TB/s).  Taken by the
 // owners of dq instead, the owners of dk and dv would have to wait for them.
+// float16: the sums of |do| too, and ahead of the rows' workgroups the `of_v` of
+// the states' largest values (8 x 3136 x 8 heads of 128 components: 10 us more).
 template <class Tag, bool VEC>
-__global__ __launch_bounds__(256) void attn_stat_kernel(AttnArgs a) {
+__global__ __launch_bounds__(256) void attn_stat_kernel(AttnArgs a, uint32_t of_v) {
   constexpr int CE = 16 / Tag::ES;
-  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  if constexpr (kPower<Tag>) {
+    if (blockIdx.x < of_v) return take_top_v<Tag, VEC>(a, blockIdx.x);
+  }
+  const int64_t row = (int64_t)(blockIdx.x - of_v) * 16 + (threadIdx.x >> 4);
   const int lane = threadIdx.x & 15;
   if (row >= a.B * a.Hk * (int64_t)a.R) return;
   const int64_t bh = row / a.R, b = bh / a.Hk;
   const int r = (int)(row - bh * a.R), hk = (int)(bh - b * a.Hk);
   const char *o = group_row(a, a.o, b, hk, r), *g = group_row(a, a.dout, b, hk, r);
-  float d = 0.f;
-  for (int c = lane; c * CE < a.D; c += 16)
-    d += chunk_dot<Tag>(load_chunk<Tag, VEC>(o, c * CE, a.D), load_chunk<Tag, VEC>(g, c * CE, a.D));
+  float d = 0.f, n = 0.f;
+  for (int c = lane; c * CE < a.D; c += 16) {
+    const u32x4 y = load_chunk<Tag, VEC>(g, c * CE, a.D);
+    d += chunk_dot<Tag>(load_chunk<Tag, VEC>(o, c * CE, a.D), y);
+    if constexpr (kPower<Tag>) n += chunk_sum<Tag>(y);
+  }
 #pragma unroll
-  for (int m = 8; m > 0; m /= 2) d += __shfl_xor(d, m, 16);
-  if (lane == 0) a.rowstat[row] = stat_of<Tag>(a, b, hk, r, d);
+  for (int m = 8; m > 0; m /= 2) {
+    d += __shfl_xor(d, m, 16);
+    if constexpr (kPower<Tag>) n += __shfl_xor(n, m, 16);
+  }
+  if (lane == 0) {
+    a.rowstat[row] = stat_of<Tag>(a, b, hk, r, d);
+    if constexpr (kPower<Tag>) a.sum_do[row] = n;
+  }
 }
 
 // The lane's row of what attn_stat_kernel left.
@@ -1048,6 +1158,17 @@ template <class Tag> __device__ inline float2 load_stat(const AttnArgs &a, int64
   float2 st = blind_stat<Tag>();
   if (r < a.R) st = a.rowstat[bh * a.R + r];
   return st;
+}
+
+// dq's power of two for the lane's row over the states of blocks first .. end of
+// 32: into the statistics that its weights start from; returns what takes it off.
+template <class Tag>
+__device__ inline float raise_row(const AttnArgs &a, int64_t bh, int r, int first, int end, int lane, float2 *st) {
+  if constexpr (!kPower<Tag>) return 1.f;
+  const float v = wave_top(a.top_v + bh * ((a.Sk + 31) / 32), first, end, lane);
+  const int e = power_for(r < a.R ? a.sum_do[bh * a.R + r] * v : 0.f);
+  st->x += (float)(e - kRaiseBack<Tag>) / a.c;
+  return exponent(-e);
 }
 
 // (The value is made anew each time: sixteen copies of it would otherwise be
@@ -1101,7 +1222,7 @@ __device__ inline void take_dq(const AttnArgs &a, char *smem, int64_t id, int64_
   u32x4 qf[T::NU], gf[T::NU];
   load_rows<Tag, DP, VEC>(a, a.q, b, hk, r, lane, qf);
   load_rows<Tag, DP, VEC>(a, a.dout, b, hk, r, lane, gf);
-  const float2 st = load_stat<Tag>(a, bh, r);
+  float2 st = load_stat<Tag>(a, bh, r);
   const char *kb = a.k.p + b * a.k.b + hk * a.k.h, *vb = a.v.p + b * a.v.b + hk * a.v.h;
   const uint8_t *mask = !PLAIN && a.mask ? a.mask + b * a.mask_b : nullptr;
   StateMover<Tag, DP, VEC, F::BN, 256> mk, mv;
@@ -1121,6 +1242,7 @@ __device__ inline void take_dq(const AttnArgs &a, char *smem, int64_t id, int64_
   };
   if constexpr (VEC) Direct::clear(smem, 4, a.D, tid);
   if (t1 > 0) load(0);
+  const float lower = raise_row<Tag>(a, bh, r, 0, (len + 31) / 32, lane, &st);
   arrived(qf);
   arrived(gf);
   for (int t = 0; t < t1; ++t) {
@@ -1220,7 +1342,7 @@ __device__ inline void take_dq(const AttnArgs &a, char *smem, int64_t id, int64_
     __syncthreads();
     if (wk > 0) return;
   }
-  store_rows<Tag, DP, VEC>(smem + wave * 32 * T::PITCH, acc, a.scale, a.D, lane,
+  store_rows<Tag, DP, VEC>(smem + wave * 32 * T::PITCH, acc, a.scale * lower, a.D, lane,
                            [&](int n) { return group_row(a, a.dq, b, hk, rt * F::BM + wr * 32 + n); });
 }
 
@@ -1251,7 +1373,7 @@ __device__ inline void take_few_dq(const AttnArgs &a, char *smem, int64_t id, in
   const uint8_t *mask = a.mask ? a.mask + b * a.mask_b : nullptr;
   load_rows<Tag, DP, VEC>(a, a.q, b, hk, rt * 32 + l31, lane, qf);
   load_rows<Tag, DP, VEC>(a, a.dout, b, hk, rt * 32 + l31, lane, gf);
-  const float2 st = load_stat<Tag>(a, bh, rt * 32 + l31);
+  float2 st = load_stat<Tag>(a, bh, rt * 32 + l31);
   const int kt = wave * F::TILE;
   uint32_t sight = 1;
   const int rowlane = T::rowlane(lane), collane = T::collane(lane);
@@ -1262,6 +1384,7 @@ __device__ inline void take_few_dq(const AttnArgs &a, char *smem, int64_t id, in
     load_states<Tag, DP, VEC>(vb, a.v.s, t * 32, len, a.D, lane, vf);
     sight = load_sight(mask, a.mask_s, t * 32, 32, len, lane);
   }
+  const float lower = raise_row<Tag>(a, bh, rt * 32 + l31, t0, t1, lane, &st);
   for (; t < t1; t += 4) {
     uint32_t see = 0xffffffffu;
     if (mask || (t + 1) * 32 > len) see = (uint32_t)sight_bits(sight, t * 32, 32, len, lane);
@@ -1288,6 +1411,10 @@ __device__ inline void take_few_dq(const AttnArgs &a, char *smem, int64_t id, in
     const Weights<Tag> w = to_weights<Tag>(s);
     cols_product<Tag, DP>(smem, kt + collane, 0, w, acc);
     wave_lds_fence();
+  }
+  if constexpr (kPower<Tag>) {
+#pragma unroll
+    for (int d = 0; d < DT; ++d) acc[d] *= lower;
   }
   float *xo = (float *)smem;
   __syncthreads();
@@ -1433,6 +1560,18 @@ __device__ inline void take_dkv(const AttnArgs &a, char *smem, int64_t id, int64
   f32x16 dk[DT] = {}, dv[DT] = {};
   if constexpr (VEC) DirectTile<Tag, DP, F::BR, PLAIN>::clear(smem, 4, a.D, tid);
   if (t0 < t1) load(t0);
+  // the power of two of ds, beside that of the weights, and what takes both off
+  float up = 1.f, lower = 1.f;
+  if constexpr (kPower<Tag>) {
+    u16x2 top = {0, 0};
+#pragma unroll
+    for (int u = 0; u < T::NU; ++u) top = chunk_top(vf[u], top);
+    const float v = other_half_max(to_f32<Tag>((u16)top_of(top)));
+    const int last = t1 * F::BR < a.R ? t1 * F::BR : a.R;
+    const int e = power_for(v * wave_top(a.sum_do + bh * a.R, t0 * F::BR, last, lane));
+    up = exponent(e - kRaiseBack<Tag>);
+    lower = exponent(-e);
+  }
   arrived(kf);
   if constexpr (!F::VLDS) arrived(vf);
   for (int t = t0; t < t1; ++t) {
@@ -1481,7 +1620,10 @@ __device__ inline void take_dkv(const AttnArgs &a, char *smem, int64_t id, int64
       };
       auto to_ds8 = [&](int t) {
 #pragma unroll
-        for (int i = 8 * t; i < 8 * t + 8; ++i) dp[i] *= s[i];
+        for (int i = 8 * t; i < 8 * t + 8; ++i) {
+          dp[i] *= s[i];
+          if constexpr (kPower<Tag>) dp[i] *= up;
+        }
       };
 #pragma unroll
       for (int n = 0; n < P; ++n) f[n] = read(n);
@@ -1523,6 +1665,7 @@ __device__ inline void take_dkv(const AttnArgs &a, char *smem, int64_t id, int64
         for (int e = 0; e < 4; ++e) {
           s[i + e] = weight<Tag>(s[i + e], a.c, x[e]);
           dp[i + e] = ds_of<Tag>(s[i + e], dp[i + e], y[e]);
+          if constexpr (kPower<Tag>) dp[i + e] *= up;
         }
       }
       cols_product<Tag, DP>(smem, gt + collane, 0, to_weights<Tag>(s), dv);
@@ -1535,18 +1678,19 @@ __device__ inline void take_dkv(const AttnArgs &a, char *smem, int64_t id, int64
     for (int d = 0; d < DT; ++d) dk[d] = dv[d] = (f32x16){};
   }
   __syncthreads();
+  const float fk = a.scale * lower, fv = exponent(-kRaiseBack<Tag>);
   if (a.row_parts > 1) {
     float *pk = a.part_dk + (part * a.B * a.Hk + bh) * a.Sk * a.D, *pv = a.part_dv + (pk - a.part_dk);
     auto row = [&](float *p, int n) { return j0 + n < a.Sk ? (char *)(p + (int64_t)(j0 + n) * a.D) : nullptr; };
-    store_rows<TagF32, DP, VEC>(smem + wave * F::OUT, dk, a.scale, a.D, lane, [&](int n) { return row(pk, n); });
-    store_rows<TagF32, DP, VEC>(smem + wave * F::OUT, dv, 1.f, a.D, lane, [&](int n) { return row(pv, n); });
+    store_rows<TagF32, DP, VEC>(smem + wave * F::OUT, dk, fk, a.D, lane, [&](int n) { return row(pk, n); });
+    store_rows<TagF32, DP, VEC>(smem + wave * F::OUT, dv, fv, a.D, lane, [&](int n) { return row(pv, n); });
     return;
   }
   auto row = [&](const Tokens &t, int n) {
     return j0 + n < a.Sk ? t.p + b * t.b + (j0 + n) * t.s + hk * t.h : nullptr;
   };
-  store_rows<Tag, DP, VEC>(smem + wave * F::OUT, dk, a.scale, a.D, lane, [&](int n) { return row(a.dk, n); });
-  store_rows<Tag, DP, VEC>(smem + wave * F::OUT, dv, 1.f, a.D, lane, [&](int n) { return row(a.dv, n); });
+  store_rows<Tag, DP, VEC>(smem + wave * F::OUT, dk, fk, a.D, lane, [&](int n) { return row(a.dk, n); });
+  store_rows<Tag, DP, VEC>(smem + wave * F::OUT, dv, fv, a.D, lane, [&](int n) { return row(a.dv, n); });
 }
 
 // dq and dk, dv in one launch: the owners of states take the first `n_dkv`
@@ -1591,7 +1735,8 @@ struct RowsShape {
   static constexpr int Q = 0, G = ROWS * PITCH, STAT = 2 * ROWS * PITCH;
   static constexpr int DS = 32 * Tile<Tag, 32>::PITCH;  // a wave's ds: 32 states of 32 rows
   static constexpr int WAVE = 2 * 32 * PITCH + DS;      // a wave's keys, values and ds
-  static constexpr int W0 = STAT + 2 * ROWS * 4;
+  static constexpr int NORM = STAT + 2 * ROWS * 4;      // float16: the waves' largest sums of |do|
+  static constexpr int W0 = NORM + (kPower<Tag> ? 256 : 0);
   static constexpr int JOIN = 3 * NRB * 16 * (DP / 32) * 64 * 4;
   static constexpr int LDS = W0 + 4 * WAVE > JOIN ? W0 + 4 * WAVE : JOIN;
 };
@@ -1648,6 +1793,15 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
 #pragma unroll
       for (int u = 0; u < NU; ++u) d += chunk_dot<Tag>(of[u], gf[u]);
       d = other_half_sum(d);
+      if constexpr (kPower<Tag>) {
+        float n = 0.f;
+#pragma unroll
+        for (int u = 0; u < NU; ++u) n += chunk_sum<Tag>(gf[u]);
+        n = other_half_sum(n);
+        // (a row that is not finite makes its own gradients what they are)
+        const uint32_t most = wave_max(n < INFINITY ? __float_as_uint(n) : 0);
+        if (lane == 0) ((uint32_t *)(smem + F::NORM))[wave] = most;
+      }
       const float2 st = r < a.R ? stat_of<Tag>(a, b, hk, r, d) : blind_stat<Tag>();
       if (h == 0) {
         ((float *)(smem + F::STAT))[r] = st.x;
@@ -1658,6 +1812,14 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
   __syncthreads();
 
   f32x16 dq[F::NRB][DT] = {};
+  // float16's power of two: of all rows together, since the same ds serves dk
+  // and dq; lowered where a block of states has larger values than those before
+  float sum_do = 0.f;
+  int power = 100;
+  if constexpr (kPower<Tag>) {
+#pragma unroll
+    for (int n = 0; n < F::NRB; ++n) sum_do = fmaxf(sum_do, ((const float *)(smem + F::NORM))[n]);
+  }
   for (; t < t1; t += 4) {
     const int j0 = t * 32;
     f32x16 dk[DT] = {}, dv[DT] = {};
@@ -1671,6 +1833,22 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
       mv.store(smem + vt, lane);
       if (t + 4 < t1) load(t + 4);
       wave_lds_fence();
+      if constexpr (kPower<Tag>) {
+        // (read back from LDS: from the registers it made others spill)
+        u16x2 top = {0, 0};
+#pragma unroll
+        for (int p = 0; p < StateMover<Tag, DP, VEC, 32, 64>::NP; ++p)
+          top = chunk_top(*(const u32x4 *)(smem + vt + p * 1024 + lane * 16), top);
+        const float bound = to_f32<Tag>((u16)wave_max(top_of(top))) * sum_do;
+        const int e = __builtin_amdgcn_readfirstlane(power_for(bound));
+        const int low = e < power ? e : power;
+        const float fix = power - low < 126 ? exponent(low - power) : 0.f;
+        power = low;
+#pragma unroll
+        for (int n = 0; n < F::NRB; ++n)
+#pragma unroll
+          for (int d = 0; d < DT; ++d) dq[n][d] *= fix;
+      }
 #pragma unroll
       for (int rb = 0; rb < F::NRB; ++rb) {
         if (rb >= nrb) continue;
@@ -1695,6 +1873,7 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
         for (int i = 0; i < 16; ++i) {
           s[i] = exp2_(s[i] * a.c);
           dp[i] *= s[i];
+          if constexpr (kPower<Tag>) dp[i] *= exponent(power - kRaiseBack<Tag>);
         }
         // p and ds are rounded to the inputs' type for their products
         const Weights<Tag> wd = to_weights<Tag>(dp);
@@ -1720,14 +1899,16 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
     auto row = [&](const Tokens &o, int n) {
       return j0 + n < a.Sk ? o.p + b * o.b + (j0 + n) * o.s + hk * o.h : nullptr;
     };
-    store_rows<Tag, DP, VEC>(smem + vt, dv, 1.f, a.D, lane, [&](int n) { return row(a.dv, n); });
-    store_rows<Tag, DP, VEC>(smem + kt, dk, a.scale, a.D, lane, [&](int n) { return row(a.dk, n); });
+    const float fk = kPower<Tag> ? a.scale * exponent(-power) : a.scale;
+    store_rows<Tag, DP, VEC>(smem + vt, dv, exponent(-kRaiseBack<Tag>), a.D, lane, [&](int n) { return row(a.dv, n); });
+    store_rows<Tag, DP, VEC>(smem + kt, dk, fk, a.D, lane, [&](int n) { return row(a.dk, n); });
   }
 
-  // the waves' parts of dq
+  // the waves' parts of dq, without their powers of two
   __syncthreads();
   float *xo = (float *)smem;  // [wave - 1][16 NRB DT][64]
   constexpr int PER = 16 * F::NRB * DT * 64;
+  const float lower = exponent(kPower<Tag> ? -power : 0);
   if (wave > 0) {
     float *o = xo + (wave - 1) * PER + lane;
 #pragma unroll
@@ -1735,7 +1916,7 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) o[((rb * DT + d) * 16 + i) * 64] = dq[rb][d][i];
+        for (int i = 0; i < 16; ++i) o[((rb * DT + d) * 16 + i) * 64] = dq[rb][d][i] * lower;
   }
   __syncthreads();
   if (wave > 0) return;
@@ -1745,7 +1926,7 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
     for (int d = 0; d < DT; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
-        float x = dq[rb][d][i];
+        float x = dq[rb][d][i] * lower;
 #pragma unroll
         for (int w = 0; w < 3; ++w) x += xo[w * PER + ((rb * DT + d) * 16 + i) * 64 + lane];
         dq[rb][d][i] = x;
@@ -1862,7 +2043,12 @@ hipError_t launch_bwd(const AttnArgs &a, hipStream_t stream) {
     }
   }
   const int64_t rows = bh * a.R;
-  if (rows > 0) WBMM_ATTN_LAUNCH((attn_stat_kernel<Tag, VEC>), (rows + 15) / 16, 0, a);
+  if (rows > 0) {
+    const int64_t of_v = kPower<Tag> ? bh * ((a.Sk + 127) / 128) : 0;
+    attn_stat_kernel<Tag, VEC><<<dim3((unsigned)(of_v + (rows + 15) / 16)), dim3(256), 0, stream>>>(a, (uint32_t)of_v);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   if (a.tile_rows == 32)
     launch_grads<Tag, DP, 0, VEC, false>(a, FewShape<Tag, DP>::lds(a.R), stream);
   else if (a.tile_rows == 64)

@@ -180,7 +180,7 @@ int64_t up16(int64_t n) { return (n + 15) / 16 * 16; }
 
 // Space of a planned call.
 struct Space {
-  int64_t part_o, part_l, part_dk, part_dv, total;
+  int64_t sum_do, top_v, part_o, part_l, part_dk, part_dv, total;
 };
 Space forward_space(const AttnArgs &a) {
   Space w = {};
@@ -193,7 +193,10 @@ Space forward_space(const AttnArgs &a) {
 }
 Space backward_space(const AttnArgs &a) {
   Space w = {};
-  w.part_o = a.one_pass ? 0 : up16(a.B * a.Hk * (int64_t)a.R * 8);
+  const int64_t bh = a.B * a.Hk;
+  w.sum_do = a.one_pass ? 0 : up16(bh * a.R * 8);
+  w.top_v = w.sum_do + (a.powers ? up16(bh * a.R * 4) : 0);
+  w.part_o = w.top_v + (a.powers ? up16(bh * ((a.Sk + 31) / 32) * 4) : 0);
   const int64_t dq = a.splits > 1 ? up16((int64_t)a.splits * a.B * a.Hk * a.R * a.D * 4) : 0;
   const int64_t part = a.row_parts > 1 ? up16((int64_t)a.row_parts * a.B * a.Hk * a.Sk * a.D * 4) : 0;
   w.part_dk = w.part_o + dq;
@@ -331,6 +334,8 @@ wbmm_status wbmm_cross_attention_backward(const wbmm_cross_attention_args *g, vo
         clash_any(ws, out, 3))
       return WBMM_ERR_INVALID_ARG;
     a.rowstat = (float2 *)g->workspace;
+    a.sum_do = (float *)((char *)g->workspace + w.sum_do);
+    a.top_v = (float *)((char *)g->workspace + w.top_v);
     a.part_o = (float *)((char *)g->workspace + w.part_o);
     a.part_dk = (float *)((char *)g->workspace + w.part_dk);
     a.part_dv = (float *)((char *)g->workspace + w.part_dv);
@@ -450,6 +455,7 @@ void attn_plan_backward(Dt dt, AttnArgs *a) {
     a->splits = (int)clamp(bh > 0 ? kUnits / bh : 1, 1, clamp(a->Sk / 96, 1, 64));
     return;
   }
+  a->powers = dt == Dt::F16;
   const int wide = (a->D + 31) / 32 * 32;
   if (dt == Dt::F32)
     plan_by({3, 7.4, 0.98, {1.13, 1.37, 1.13}, 50e-3 * (wide + 16), 5}, true, a);

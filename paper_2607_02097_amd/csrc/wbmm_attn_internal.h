@@ -54,9 +54,12 @@ struct AttnArgs {
   // and, forward, part_l [splits, B Hk, R] (lse in log2 units).
   int tile_rows, splits;
   int one_pass;  // backward: one kernel for all gradients, of `splits` parts
+  int powers;    // backward: sum_do and top_v are taken
   float *part_o, *part_l;
-  // backward: two statistics per row, [B Hk, R] (row_stat)
+  // backward: two statistics per row, [B Hk, R]; for float16's powers of two
+  // sums of |dout| per row and the largest |v| of 32 states, [B Hk, ceil(Sk / 32)]
   float2 *rowstat;
+  float *sum_do, *top_v;
   // backward: dk, dv in `row_parts` parts of the rows, with partial sums
   // part_dk, part_dv [row_parts, B Hk, Sk, D]
   int row_parts;

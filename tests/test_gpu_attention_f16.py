@@ -1,0 +1,153 @@
+"""Gradients of the cross attention in float16 whose weights and their
+gradients lie far below, or above, the type's normal range.
+
+p and ds are rounded to float16 as operands of the second products.  Each of
+these roundings is off by at most u = 2^-11 of its value, independently of the
+others, so the root mean square of what they make of a sum is at most
+u sqrt(sum (ds k)^2).  The products are taken with powers of two that keep the
+operands in the normal range: weights 2^12 larger (2^-37 of absolute
+precision), ds by a bound B, the largest sum |dout| of the rows times the
+largest |v| of the states, so that half a smallest step is 2^-38 B.  delta
+comes from the rounded out, off by u sqrt(sum (dout out)^2) for all states of
+a row at once.  The result is rounded once more: u of itself, or half of
+float16's smallest step, 2^-25.  Twice the sum of squares' root is allowed for
+the first two (the roundings of float32 are a thousand times smaller).
+"""
+import pytest
+import torch
+
+from paper_2607_02097_amd import binding as W
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -11
+
+
+def draw(shape, seed, std=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(shape, generator=g, dtype=torch.float64) * std).half()
+
+
+def plain(q, k, v, g, scale):
+    """64-bit gradients, and the mean squares of their errors by the head of
+    this file."""
+    B, Sq, Hq, D = q.shape
+    Hk = k.shape[2]
+    G = Hq // Hk
+    grads = [torch.zeros(t.shape, dtype=torch.float64) for t in (q, k, v)]
+    square = [torch.zeros(t.shape, dtype=torch.float64) for t in (q, k, v)]
+    for b in range(B):
+        for j in range(Hk):
+            K, V = k[b, :, j].double(), v[b, :, j].double()
+            most = g[b, :, j * G:(j + 1) * G].double().abs().sum(-1).max() * V.abs().max()
+            parts = []
+            for h in range(j * G, (j + 1) * G):
+                Q, dO = q[b, :, h].double(), g[b, :, h].double()
+                p = torch.softmax(scale * (Q @ K.T), -1)
+                o = p @ V
+                ds = p * (dO @ V.T - (dO * o).sum(-1, keepdim=True))
+                parts.append((h, Q, dO, p, o, ds))
+            for h, Q, dO, p, o, ds in parts:
+                e2 = (U * ds) ** 2 + (2.0 ** -38 * most) ** 2
+                delta2 = U ** 2 * (dO * o).square().sum(-1, keepdim=True)
+                grads[0][b, :, h] = scale * ds @ K
+                square[0][b, :, h] = scale ** 2 * (e2 @ K ** 2 + delta2 * (p @ K) ** 2)
+                grads[1][b, :, j] += scale * ds.T @ Q
+                square[1][b, :, j] += scale ** 2 * (e2.T @ Q ** 2 + (p ** 2 * delta2).T @ Q ** 2)
+                grads[2][b, :, j] += p.T @ dO
+                square[2][b, :, j] += ((U * p) ** 2 + 2.0 ** -74).T @ dO ** 2
+    return grads, square
+
+
+def compare(q, k, v, g, scale=None):
+    dev = [t.cuda() for t in (q, k, v, g)]
+    out, lse = W.wbmm_cross_attention_forward(*dev[:3], scale=scale)
+    got = W.wbmm_cross_attention_backward(dev[3], *dev[:3], out, lse, scale=scale)
+    grads, square = plain(q, k, v, g, q.shape[3] ** -0.5 if scale is None else scale)
+    for name, t, want, s2 in zip(("dq", "dk", "dv"), got, grads, square):
+        assert want.abs().max() < 65000, name  # (the case's own sizes)
+        err = (t.cpu().double() - want).square().mean().sqrt().item()
+        limit = 2 * s2.mean().sqrt().item() + torch.maximum(U * want.abs(), torch.tensor(2.0 ** -25).double()).square().mean().sqrt().item()
+        assert err <= limit, "%s: %.3g of the bound (%.2g of the result)" % (name, err / limit, err / want.square().mean().sqrt())
+
+
+SHAPES = [
+    # B, Sq, Sk, Hq, Hk, D
+    (1, 3, 6000, 2, 1, 64),      # few rows
+    (1, 30, 3000, 1, 1, 128),
+    (1, 100, 3000, 1, 1, 32),
+    (1, 12, 3001, 3, 1, 37),
+    (1, 100, 4000, 2, 1, 128),   # states and rows in parts
+    (1, 70, 3000, 2, 1, 72),
+    (1, 70, 3001, 2, 1, 45),
+    (16, 100, 1500, 8, 8, 64),   # tiles of 64 and 128 rows
+    (24, 128, 1000, 8, 8, 128),
+    (24, 128, 1000, 8, 8, 96),
+    (24, 120, 700, 8, 8, 50),
+]
+
+
+@pytest.mark.parametrize("std", [1.0, 1e-2, 1e-3, 1e-5])
+@pytest.mark.parametrize("B,Sq,Sk,Hq,Hk,D", SHAPES)
+def test_small_upstream_gradients(B, Sq, Sk, Hq, Hk, D, std):
+    """A loss averaged over many tokens, without a loss scale.  (Keys large
+    and queries small, so that dq is not itself below float16's range.)"""
+    compare(draw((B, Sq, Hq, D), 1, 0.1), draw((B, Sk, Hk, D), 2, 15.0), draw((B, Sk, Hk, D), 3), draw((B, Sq, Hq, D), 4, std))
+
+
+@pytest.mark.parametrize("falling", [False, True])
+@pytest.mark.parametrize("B,Sq,Sk,Hq,Hk,D", SHAPES)
+def test_gradients_that_grow_along_states_and_rows(B, Sq, Sk, Hq, Hk, D, falling):
+    """ds grows (or falls) by 2^16 along the states and by 2^8 along the rows,
+    so that the powers of two have to move again and again."""
+    v, g = draw((B, Sk, Hk, D), 13), draw((B, Sq, Hq, D), 14)
+    v = (v.double() * torch.logspace(-10, 6, Sk, 2.0, dtype=torch.float64)[None, :, None, None]).half()
+    g = (g.double() * torch.logspace(-8, 0, Sq, 2.0, dtype=torch.float64)[None, :, None, None]).half()
+    if falling:
+        v, g = v.flip(1), g.flip(1)
+    compare(draw((B, Sq, Hq, D), 11, 0.1), draw((B, Sk, Hk, D), 12, 10.0), v, g)
+
+
+@pytest.mark.parametrize("Sq,D", [(3, 32), (40, 64), (90, 128), (150, 64), (50, 37)])
+def test_gradients_of_weights_above_the_range(Sq, D):
+    """ds past 65504, as a large loss scale makes it, with results within."""
+    q, k = draw((2, Sq, 2, D), 21), draw((2, 40, 2, D), 22, 0.01)
+    compare(q * 0.01, k, draw((2, 40, 2, D), 23, 200.0), draw((2, Sq, 2, D), 24, 2000.0), scale=0.02)
+
+
+@pytest.mark.parametrize("B,Sq,Sk,Hq,Hk,D", [s for s in SHAPES if s[4] < 8] + [(24, 120, 200, 8, 8, 64), (24, 65, 200, 8, 8, 50)])
+def test_powers_do_not_depend_on_hidden_states(B, Sq, Sk, Hq, Hk, D):
+    """Hidden states may hold anything, the type's largest numbers too: the
+    same bits as with zeros there."""
+    q, k, v, g = (draw(s, i, e).cuda() for i, (s, e) in enumerate(
+        (((B, Sq, Hq, D), 0.2), ((B, Sk, Hk, D), 3.0), ((B, Sk, Hk, D), 1e-2), ((B, Sq, Hq, D), 1e-3)), 31))
+    mask = torch.rand((B, Sk), generator=torch.Generator().manual_seed(35)).cuda() < 0.6
+    mask[:, 64:160] = False
+    lens = torch.full((B,), Sk - 37, dtype=torch.int32, device="cuda")
+    see = mask & (torch.arange(Sk, device="cuda") < Sk - 37)
+    results = []
+    for fill in (0.0, 65504.0, float("inf"), float("nan")):
+        k2, v2 = k.clone(), v.clone()
+        k2[~see], v2[~see] = fill, fill
+        out, lse = W.wbmm_cross_attention_forward(q, k2, v2, lens, mask)
+        results.append((out, lse) + W.wbmm_cross_attention_backward(g, q, k2, v2, out, lse, lens, mask))
+    assert results[0][2].abs().max() > 0
+    for other in results[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(results[0], other))
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")])
+@pytest.mark.parametrize("B,Sq,Sk,Hq,Hk,D", SHAPES)
+def test_powers_do_not_depend_on_rows_that_are_not_finite(B, Sq, Sk, Hq, Hk, D, bad):
+    """A row whose upstream gradient overflowed leaves the other rows' dq as
+    it is with zeros there."""
+    q, k, v, g = (draw(s, i, e).cuda() for i, (s, e) in enumerate(
+        (((B, Sq, Hq, D), 0.2), ((B, Sk, Hk, D), 3.0), ((B, Sk, Hk, D), 1.0), ((B, Sq, Hq, D), 1e-3)), 41))
+    out, lse = W.wbmm_cross_attention_forward(q, k, v)
+    g[0, 1, 0] = 0.0
+    clean = W.wbmm_cross_attention_backward(g, q, k, v, out, lse)[0]
+    g[0, 1, 0, 2] = bad
+    dq = W.wbmm_cross_attention_backward(g, q, k, v, out, lse)[0]
+    others = torch.ones(B, Sq, Hq, dtype=torch.bool, device="cuda")
+    others[0, 1, 0] = False
+    assert torch.equal(dq[others], clean[others]) and not bool(dq[~others].isfinite().any())
