@@ -1602,10 +1602,10 @@ __device__ inline void take_dkv(const AttnArgs &a, char *smem, int64_t id, int64
         for (int e = 0; e < 4; ++e) s[i + e] = x[e], dp[i + e] = y[e];
       }
     }
-    if constexpr (Tag::W16 && VEC && F::VLDS) {
+    if constexpr (VEC && F::VLDS) {
       // One stream of fragment reads, some products ahead of their use: queries
-      // for the scores, do (and the values, where they are in LDS) for dp, while
-      // which the weights are formed, then the columns of do and of the queries.
+      // for the scores, do and the values for dp, while which the weights are
+      // formed, then the columns of do and of the queries.
       constexpr int NU = T::NU, N = 2 * NU + 4 * DT, P = 4, PV = 2;
       u32x4 f[P], v[PV], w[2];
       auto read = [&](int n) {
@@ -1638,13 +1638,13 @@ __device__ inline void take_dkv(const AttnArgs &a, char *smem, int64_t id, int64
         if (n < NU)
           s = mma_chunk<Tag>(f[n % P], kf[n], s);
         else if (n < 2 * NU)
-          dp = mma_chunk<Tag>(f[n % P], F::VLDS ? v[n % PV] : vf[F::VLDS ? 0 : n - NU], dp);
+          dp = mma_chunk<Tag>(f[n % P], v[n % PV], dp);
         else if (m < 2 * DT)
           dv[m % DT] = mma_chunk<Tag>(f[n % P], w[m / DT], dv[m % DT]);
         else
           dk[m % DT] = mma_chunk<Tag>(f[n % P], w[m / DT - 2], dk[m % DT]);
         if (n + P < N) f[n % P] = read(n + P);
-        if (F::VLDS && n + PV >= NU && n + PV < 2 * NU) v[n % PV] = *(const u32x4 *)(smem + (val ^ ((n + PV) % NU << 5)));
+        if (n + PV >= NU && n + PV < 2 * NU) v[n % PV] = *(const u32x4 *)(smem + (val ^ ((n + PV) % NU << 5)));
         if (n >= NU && n < 2 * NU) {
 #pragma unroll
           for (int i = (n - NU) * 16 / NU; i < (n - NU + 1) * 16 / NU; ++i) s[i] = exp2_(s[i] * a.c);
