@@ -304,7 +304,8 @@ typedef struct {
  * of axis a by the angle t = positions[a][b][s] * freqs[i]:
  *   lo' = lo cos t - hi sin t,  hi' = lo sin t + hi cos t
  * Components from 2 P on are copied.  The angle is taken in 64 bits (exact for
- * positions below 2^29), the rotation in float32, each output rounded once.
+ * positions below 2^29), its cosine and sine in float32 to within 3 x 2^-23 of
+ * themselves, the rotation in float32, each output rounded once.
  * positions: device, 32- or 64-bit integers (position_bytes 4 or 8) at any
  * strides, 0 for a broadcast; freqs: device, float32 [P], radians a position.
  * 1 <= axes <= 4, sections not negative, 1 <= P <= 256, 2 P <= D <= 4096.

@@ -12,6 +12,10 @@
 // for all heads; then its threads stream the heads' components in 16-byte
 // pieces.  The angle is taken in 64 bits and reduced to a fraction of a turn
 // there, since in 32 bits a position of 2^20 leaves no more than 2^-4 radians.
+// Cosine and sine are taken in float32, of the fraction rounded to float32, and
+// turned by what that left: float32 results are off by 0.69 x 2^-24 of themselves
+// (root mean square), without it by 0.90, from cosines and sines of 64 bits that
+// are rounded once by 0.71.
 // Measured: 12544 x 40 x 128 bfloat16 39.7 us (6.5 TB/s); eight tokens 4 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -161,10 +165,13 @@ __global__ __launch_bounds__(kRotThreads) void rotary_kernel(RotaryArgs a, RotPl
     const int64_t pa = axis * a.pos_a + b * a.pos_b + s * a.pos_s;
     const double p = a.pos64 ? (double)((const int64_t *)a.pos)[pa] : (double)((const int32_t *)a.pos)[pa];
     const double turns = p * (double)a.freqs[i] * 0.15915494309189533577;
-    const float half = (float)(2.0 * (turns - rint(turns)));  // half turns, -1 .. 1
+    const double exact = 2.0 * (turns - rint(turns));  // half turns, -1 .. 1
+    const float half = (float)exact, rest = (float)((exact - (double)half) * 3.14159265358979323846);
     float sn, cn;
     sincospif(half, &sn, &cn);
-    cs[e] = make_float2(cn, a.reverse ? -sn : sn);
+    const float s1 = __builtin_fmaf(cn, rest, sn);  // (|rest| < 2^-23)
+    cn = __builtin_fmaf(-sn, rest, cn);
+    cs[e] = make_float2(cn, a.reverse ? -s1 : s1);
   }
   __syncthreads();
   for (int g0 = tid; g0 < items; g0 += U * kRotThreads) {
