@@ -336,8 +336,9 @@ wbmm_status wbmm_rotary_backward(const wbmm_rotary_args *args, void *stream);
  * values are clamped to 0..Sk) and key_mask[b, j] is not zero (device, one
  * byte each, element strides mask_stride_b and mask_stride_s, or NULL: all).
  * What lies in states that are not visible may be anything, NaN included.
- * Where nothing is visible, out = 0, lse = -infinity and all gradients are 0;
- * gradients of states that are not visible are 0.
+ * Where nothing is visible (or all visible scores are -infinity), out = 0, lse =
+ * -infinity and all gradients are 0; gradients of states that are not visible
+ * are 0.
  * q, out, dout, dq: [B,Sq,Hq,D]; k, v, dk, dv: [B,Sk,Hk,D]; lse: float32
  * [B,Hq,Sq] contiguous.  1 <= D <= 128; 1e-30 <= scale, finite.  B, Sq and
  * Sk may be 0.  16-bit types: products on the matrix cores with float32

@@ -989,7 +989,9 @@ __global__ __launch_bounds__(256) void attn_join_kernel(AttnArgs a) {
 // ds = p (do.v - delta):  dq = scale ds K,  dk = scale ds^T Q,  dv = p^T do.
 // The scores are recomputed twice, by the owners of rows for dq and by the
 // owners of states for dk and dv, so every sum has one owner and a fixed order:
-// no atomics, and the same bits every time.
+// no atomics, and the same bits every time.  In 16 bits delta is that of the
+// rounded out (a float32 out would be an output more), off by half a step of
+// each of its components, and p and ds are rounded for the matrix cores.
 
 // Statistics of the lane's row.  16-bit: what its products start from,
 // {-lse / scale, -delta}, so that they come out as the weight's exponent and as

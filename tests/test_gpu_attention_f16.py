@@ -151,3 +151,23 @@ def test_powers_do_not_depend_on_rows_that_are_not_finite(B, Sq, Sk, Hq, Hk, D, 
     others = torch.ones(B, Sq, Hq, dtype=torch.bool, device="cuda")
     others[0, 1, 0] = False
     assert torch.equal(dq[others], clean[others]) and not bool(dq[~others].isfinite().any())
+
+
+@pytest.mark.parametrize("B,Sq,Sk,Hq,Hk,D", [(1, 3, 6000, 2, 1, 64), (1, 100, 4000, 2, 1, 128), (24, 120, 700, 8, 8, 50)])
+def test_captured_gradients(B, Sq, Sk, Hq, Hk, D):
+    """Gradients replayed from a graph, between eager calls on other sizes of
+    dout, whose powers of two differ."""
+    q, k, v, g = (draw(s, i, e).cuda() for i, (s, e) in enumerate(
+        (((B, Sq, Hq, D), 0.2), ((B, Sk, Hk, D), 3.0), ((B, Sk, Hk, D), 1.0), ((B, Sq, Hq, D), 1e-3)), 51))
+    out, lse = W.wbmm_cross_attention_forward(q, k, v)
+    W.wbmm_cross_attention_backward(g, q, k, v, out, lse)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        caught = W.wbmm_cross_attention_backward(g, q, k, v, out, lse)
+    for std in (1e-3, 100.0, 1.0, 1e-4):
+        g.copy_(draw(g.shape, 55, std))
+        graph.replay()
+        eager = W.wbmm_cross_attention_backward(g, q, k, v, out, lse)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(caught, eager)) and bool(caught[0].abs().max() > 0)
