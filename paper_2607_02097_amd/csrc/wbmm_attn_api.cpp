@@ -450,8 +450,7 @@ void attn_plan_forward(Dt dt, AttnArgs *a) {
 
 // Few rows (16-bit): all gradients in one pass over the states, in parts for a
 // workgroup on every unit: 64 key heads of 128 components over 3136 states
-// 114 us in one part, 49 in four (one workgroup a unit), 60 in eight; 192
-// heads 24 us in one part, 26 in two.
+// 114 us in one part, 49 in four (one workgroup a unit), 60 in eight.
 void attn_plan_backward(Dt dt, AttnArgs *a) {
   const int64_t bh = a->B * a->Hk;
   if (dt != Dt::F32 && a->R > 0 && a->R <= one_pass_rows(a->D) && a->Sk > 0) {

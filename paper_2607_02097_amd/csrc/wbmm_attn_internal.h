@@ -71,9 +71,8 @@ struct AttnArgs {
 // beside dk and dv of a block.  Twice the rows need the registers of two waves
 // or spill, and were slower: 1024 heads of 128 components, 64 rows, 784 states
 // 772 us against 333 in separate kernels; 64 components, 128 rows 203 against 202;
-// 32 components, 100 rows 69 against 99.  The largest instances spill as they
-// are: 128 components 61 registers of 512 (at one wave a SIMD), 64 components of
-// 64 rows 9 of 256.
+// 32 components, 100 rows 69 against 99.  64 components of 64 rows spill
+// 9 registers of 256 as it is.
 constexpr int one_pass_rows(int D) { return D <= 32 ? 128 : D <= 64 ? 64 : 32; }
 
 template <class Tag>
