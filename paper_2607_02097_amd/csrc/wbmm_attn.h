@@ -1710,8 +1710,8 @@ __device__ inline void take_dkv(const AttnArgs &a, char *smem, int64_t id, int64
 // their own.  Measured against kernels one after the other (the first taking
 // the rows' statistics on its way), bfloat16: 2 x 8 heads of 200 queries over
 // 1001 states of 64 components 24 -> 19 us; float16, 12 x 6 heads of 333 over
-// 1001 masked states of 72 components 79 -> 56; 8 x 32 heads of 2048 over 6272
-// of 128 components 2685 -> 2652.
+// 1001 masked states of 72 components 79 -> 56 (60 with its powers of two); 8 x
+// 32 heads of 2048 over 6272 of 128 components 2685 -> 2652.
 template <class Tag, int DP, int WK, bool VEC, bool PLAIN>
 __global__ __launch_bounds__(256, Tag::W16 ? (DP <= 32 ? 4 : DP <= 64 ? 3 : 2) : DP <= 64 ? 2 : 1) void attn_grads_kernel(AttnArgs a, int n_dq, int n_dkv,
                                                                                       int dq_first) {

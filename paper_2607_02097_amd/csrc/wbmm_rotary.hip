@@ -16,7 +16,7 @@
 // turned by what that left: float32 results are off by 0.69 x 2^-24 of themselves
 // (root mean square), without it by 0.90, from cosines and sines of 64 bits that
 // are rounded once by 0.71.
-// Measured: 12544 x 40 x 128 bfloat16 39.7 us (6.5 TB/s); eight tokens 4 us.
+// Measured: 12544 x 40 x 128 bfloat16 40.7 us (6.3 TB/s); eight tokens 4 us.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
