@@ -1042,11 +1042,11 @@ template <class Tag> __device__ inline float2 stat_of(const AttnArgs &a, int64_t
 // a power of two on its way to the product, taken from a bound that is known
 // ahead,
 //   |ds_rj| <= |dp_rj| + |delta_r| <= 2 B,  B = sum |do_r| max |v|,
-// with the maxima over what shares a sum: for dq the row's own sum |do_r| and the
-// visible states, for dk the rows and the state's own values.  The largest ds
-// then lies below 2^15, and each keeps 2^-38 B of absolute precision (2^-25, half
-// of the type's smallest step, over the power), where it would need 2^-11 of
-// itself.  Powers: 2^13 over B's own power of two, at most 2^100.
+// with the maximum over all visible states, since delta comes from all of them,
+// and for dk over the rows.  The largest ds then lies below 2^15, and each keeps
+// 2^-38 B of absolute precision (2^-25, half of the type's smallest step, over
+// the power), where it would need 2^-11 of itself.  Powers: 2^13 over B's own
+// power of two, at most 2^100.
 template <class Tag> constexpr bool kPower = __is_same(Tag, TagF16);
 
 __device__ inline int power_for(float bound) {  // its exponent
@@ -1169,12 +1169,17 @@ template <class Tag> __device__ inline float2 load_stat(const AttnArgs &a, int64
   return st;
 }
 
-// dq's power of two for the lane's row over the states of blocks first .. end of
-// 32: into the statistics that its weights start from; returns what takes it off.
+// The largest |v| of the head's visible states.
+__device__ inline float head_top_v(const AttnArgs &a, int64_t bh, int len, int lane) {
+  return wave_top(a.top_v + bh * ((a.Sk + 31) / 32), 0, (len + 31) / 32, lane);
+}
+
+// dq's power of two for the lane's row: into the statistics that its weights
+// start from; returns what takes it off.
 template <class Tag>
-__device__ inline float raise_row(const AttnArgs &a, int64_t bh, int r, int first, int end, int lane, float2 *st) {
+__device__ inline float raise_row(const AttnArgs &a, int64_t bh, int r, int len, int lane, float2 *st) {
   if constexpr (!kPower<Tag>) return 1.f;
-  const float v = wave_top(a.top_v + bh * ((a.Sk + 31) / 32), first, end, lane);
+  const float v = head_top_v(a, bh, len, lane);
   const int e = power_for(r < a.R ? a.sum_do[bh * a.R + r] * v : 0.f);
   st->x += (float)(e - kRaiseBack<Tag>) / a.c;
   return exponent(-e);
@@ -1251,7 +1256,7 @@ __device__ inline void take_dq(const AttnArgs &a, char *smem, int64_t id, int64_
   };
   if constexpr (VEC) Direct::clear(smem, 4, a.D, tid);
   if (t1 > 0) load(0);
-  const float lower = raise_row<Tag>(a, bh, r, 0, (len + 31) / 32, lane, &st);
+  const float lower = raise_row<Tag>(a, bh, r, len, lane, &st);
   arrived(qf);
   arrived(gf);
   for (int t = 0; t < t1; ++t) {
@@ -1393,7 +1398,7 @@ __device__ inline void take_few_dq(const AttnArgs &a, char *smem, int64_t id, in
     load_states<Tag, DP, VEC>(vb, a.v.s, t * 32, len, a.D, lane, vf);
     sight = load_sight(mask, a.mask_s, t * 32, 32, len, lane);
   }
-  const float lower = raise_row<Tag>(a, bh, rt * 32 + l31, t0, t1, lane, &st);
+  const float lower = raise_row<Tag>(a, bh, rt * 32 + l31, len, lane, &st);
   for (; t < t1; t += 4) {
     uint32_t see = 0xffffffffu;
     if (mask || (t + 1) * 32 > len) see = (uint32_t)sight_bits(sight, t * 32, 32, len, lane);
@@ -1572,12 +1577,8 @@ __device__ inline void take_dkv(const AttnArgs &a, char *smem, int64_t id, int64
   // the power of two of ds, beside that of the weights, and what takes both off
   float up = 1.f, lower = 1.f;
   if constexpr (kPower<Tag>) {
-    u16x2 top = {0, 0};
-#pragma unroll
-    for (int u = 0; u < T::NU; ++u) top = chunk_top(vf[u], top);
-    const float v = other_half_max(to_f32<Tag>((u16)top_of(top)));
     const int last = t1 * F::BR < a.R ? t1 * F::BR : a.R;
-    const int e = power_for(v * wave_top(a.sum_do + bh * a.R, t0 * F::BR, last, lane));
+    const int e = power_for(head_top_v(a, bh, len, lane) * wave_top(a.sum_do + bh * a.R, t0 * F::BR, last, lane));
     up = exponent(e - kRaiseBack<Tag>);
     lower = exponent(-e);
   }
@@ -1744,7 +1745,7 @@ struct RowsShape {
   static constexpr int Q = 0, G = ROWS * PITCH, STAT = 2 * ROWS * PITCH;
   static constexpr int DS = 32 * Tile<Tag, 32>::PITCH;  // a wave's ds: 32 states of 32 rows
   static constexpr int WAVE = 2 * 32 * PITCH + DS;      // a wave's keys, values and ds
-  static constexpr int NORM = STAT + 2 * ROWS * 4;      // float16: the waves' largest sums of |do|
+  static constexpr int NORM = STAT + 2 * ROWS * 4;      // float16: the waves' largest sums of |do| and |delta|
   static constexpr int W0 = NORM + (kPower<Tag> ? 256 : 0);
   static constexpr int JOIN = 3 * NRB * 16 * (DP / 32) * 64 * 4;
   static constexpr int LDS = W0 + 4 * WAVE > JOIN ? W0 + 4 * WAVE : JOIN;
@@ -1808,8 +1809,13 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
         for (int u = 0; u < NU; ++u) n += chunk_sum<Tag>(gf[u]);
         n = other_half_sum(n);
         // (a row that is not finite makes its own gradients what they are)
-        const uint32_t most = wave_max(n < INFINITY ? __float_as_uint(n) : 0);
-        if (lane == 0) ((uint32_t *)(smem + F::NORM))[wave] = most;
+        const float x = __builtin_fabsf(d);
+        const uint32_t sums = wave_max(n < INFINITY ? __float_as_uint(n) : 0);
+        const uint32_t deltas = wave_max(n < INFINITY && x < INFINITY ? __float_as_uint(x) : 0);
+        if (lane == 0) {
+          ((uint32_t *)(smem + F::NORM))[wave] = sums;
+          ((uint32_t *)(smem + F::NORM))[4 + wave] = deltas;
+        }
       }
       const float2 st = r < a.R ? stat_of<Tag>(a, b, hk, r, d) : blind_stat<Tag>();
       if (h == 0) {
@@ -1823,11 +1829,15 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
   f32x16 dq[F::NRB][DT] = {};
   // float16's power of two: of all rows together, since the same ds serves dk
   // and dq; lowered where a block of states has larger values than those before
-  float sum_do = 0.f;
+  // (and all deltas)
+  float sum_do = 0.f, delta = 0.f;
   int power = 100;
   if constexpr (kPower<Tag>) {
 #pragma unroll
-    for (int n = 0; n < F::NRB; ++n) sum_do = fmaxf(sum_do, ((const float *)(smem + F::NORM))[n]);
+    for (int n = 0; n < F::NRB; ++n) {
+      sum_do = fmaxf(sum_do, ((const float *)(smem + F::NORM))[n]);
+      delta = fmaxf(delta, ((const float *)(smem + F::NORM))[4 + n]);
+    }
   }
   for (; t < t1; t += 4) {
     const int j0 = t * 32;
@@ -1855,7 +1865,7 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
         for (int p = 0; p < StateMover<Tag, DP, VEC, 32, 64>::NP; ++p)
           top = chunk_top(*(const u32x4 *)(smem + vt + p * 1024 + lane * 16), top);
         const float bound = to_f32<Tag>((u16)wave_max(top_of(top))) * sum_do;
-        const int e = __builtin_amdgcn_readfirstlane(power_for(bound));
+        const int e = __builtin_amdgcn_readfirstlane(power_for(bound > delta ? bound : delta));
         const int low = e < power ? e : power;
         const float fix = power - low < 126 ? exponent(low - power) : 0.f;
         power = low;

@@ -171,3 +171,17 @@ def test_captured_gradients(B, Sq, Sk, Hq, Hk, D):
         eager = W.wbmm_cross_attention_backward(g, q, k, v, out, lse)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(caught, eager)) and bool(caught[0].abs().max() > 0)
+
+
+@pytest.mark.parametrize("std", [1e-3, 1.0, 1e3])
+@pytest.mark.parametrize("where", ["first", "last", "every 50th"])
+@pytest.mark.parametrize("B,Sq,Sk,Hq,Hk,D", SHAPES + [(2, 20, 40, 2, 2, 64), (2, 100, 40, 2, 2, 128)])
+def test_values_in_a_few_states_only(B, Sq, Sk, Hq, Hk, D, where, std):
+    """Most states' values are zeros (or tiny): their ds is all delta, which
+    comes from the others."""
+    v = draw((B, Sk, Hk, D), 63, 1e-6)
+    v[:, ::2] = 0.0
+    at = {"first": slice(0, 3), "last": slice(Sk - 3, Sk), "every 50th": slice(7, None, 50)}[where]
+    v[:, at] = draw(v[:, at].shape, 65, 8.0)
+    # (scores of order 1, so that the few have their share of the weights)
+    compare(draw((B, Sq, Hq, D), 61, 0.1), draw((B, Sk, Hk, D), 62, 2.0), v, draw((B, Sq, Hq, D), 64, std))
