@@ -1040,18 +1040,18 @@ template <class Tag> __device__ inline float2 stat_of(const AttnArgs &a, int64_t
 // states, dout of std 1e-3: dq off by 0.0047 of itself as it is, by 0.00031 as
 // follows, where its last rounding alone makes 0.00021).  So it is multiplied by
 // a power of two on its way to the product, taken from a bound that is known
-// ahead,
-//   |ds_rj| <= |dp_rj| + |delta_r| <= 2 B,  B = sum |do_r| max |v|,
-// with the maximum over all visible states, since delta comes from all of them,
-// and for dk over the rows.  The largest ds then lies below 2^15, and each keeps
-// 2^-38 B of absolute precision (2^-25, half of the type's smallest step, over
-// the power), where it would need 2^-11 of itself.  Powers: 2^13 over B's own
-// power of two, at most 2^100.
+// ahead: with |dp_rj| <= B = sum |do_r| max |v| over all visible states (delta
+// comes from all of them), and delta_r the mean of dp_rj by p_rj,
+//   |ds_rj| = p_rj (1 - p_rj) |dp_rj - mean of the others| <= B / 2,
+// for dk with the largest of the rows.  The largest ds then lies below 2^15, and
+// each keeps 2^-40 B of absolute precision (2^-25, half of the type's smallest
+// step, over the power), where it would need 2^-11 of itself.  Powers: 2^14 over
+// the bound's own power of two, at most 2^100.
 template <class Tag> constexpr bool kPower = __is_same(Tag, TagF16);
 
 __device__ inline int power_for(float bound) {  // its exponent
   const int e = (int)(__float_as_uint(bound) >> 23) & 255;  // (255: not finite)
-  return 140 - (e > 40 ? e : 40);
+  return 141 - (e > 41 ? e : 41);
 }
 // 2^e, |e| < 127
 __device__ inline float exponent(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
@@ -1180,7 +1180,7 @@ template <class Tag>
 __device__ inline float raise_row(const AttnArgs &a, int64_t bh, int r, int len, int lane, float2 *st) {
   if constexpr (!kPower<Tag>) return 1.f;
   const float v = head_top_v(a, bh, len, lane);
-  const int e = power_for(r < a.R ? a.sum_do[bh * a.R + r] * v : 0.f);
+  const int e = power_for(r < a.R ? 0.5f * a.sum_do[bh * a.R + r] * v : 0.f);
   st->x += (float)(e - kRaiseBack<Tag>) / a.c;
   return exponent(-e);
 }
@@ -1578,7 +1578,8 @@ __device__ inline void take_dkv(const AttnArgs &a, char *smem, int64_t id, int64
   float up = 1.f, lower = 1.f;
   if constexpr (kPower<Tag>) {
     const int last = t1 * F::BR < a.R ? t1 * F::BR : a.R;
-    const int e = power_for(head_top_v(a, bh, len, lane) * wave_top(a.sum_do + bh * a.R, t0 * F::BR, last, lane));
+    const float sums = wave_top(a.sum_do + bh * a.R, t0 * F::BR, last, lane);
+    const int e = power_for(0.5f * sums * head_top_v(a, bh, len, lane));
     up = exponent(e - kRaiseBack<Tag>);
     lower = exponent(-e);
   }
@@ -1828,8 +1829,8 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
 
   f32x16 dq[F::NRB][DT] = {};
   // float16's power of two: of all rows together, since the same ds serves dk
-  // and dq; lowered where a block of states has larger values than those before
-  // (and all deltas)
+  // and dq, from |ds| <= |dp| + |delta|; lowered where a block of states has
+  // larger values than those before
   float sum_do = 0.f, delta = 0.f;
   int power = 100;
   if constexpr (kPower<Tag>) {
@@ -1865,7 +1866,7 @@ __global__ __launch_bounds__(256, DP <= 64 ? 2 : 1) void attn_rows_bwd_kernel(At
         for (int p = 0; p < StateMover<Tag, DP, VEC, 32, 64>::NP; ++p)
           top = chunk_top(*(const u32x4 *)(smem + vt + p * 1024 + lane * 16), top);
         const float bound = to_f32<Tag>((u16)wave_max(top_of(top))) * sum_do;
-        const int e = __builtin_amdgcn_readfirstlane(power_for(bound > delta ? bound : delta));
+        const int e = __builtin_amdgcn_readfirstlane(power_for(bound + delta));
         const int low = e < power ? e : power;
         const float fix = power - low < 126 ? exponent(low - power) : 0.f;
         power = low;
